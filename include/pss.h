@@ -372,6 +372,165 @@ int pss_hash_signs_host(int64_t M, int32_t Z, int32_t d, const pss_hash_params* 
  * offsets[T*B] == N.  Returns PSS_OK or PSS_ERR_INVALID_ARG. */
 int pss_validate_offsets_host(const int64_t* offsets, int64_t num_bags, int64_t N);
 
+/* ---------------------------------------------------------------------------
+ * Operators on rows: what a sequence model does with the layer's rows beside
+ * looking them up.  The conventions above (streams, errors, scratch, threads)
+ * hold for them too.
+ *
+ * Rows.  An argument of R rows of C elements is an address and a stride: row r
+ *   begins at element r * stride, its elements are consecutive.  float32 or
+ *   bfloat16 (pss_rows_params.dtype), any alignment of whole elements.  The
+ *   pooled rows [B][T*d] of pss_forward are B rows of T*d elements, or B rows
+ *   of d elements with stride T*d (one table), or B*T rows of d.  An input may
+ *   have any stride >= 0 (0: every row the same); an output with R > 1 needs
+ *   stride >= C.  An output may be the very array of an input row argument of
+ *   the same call (same address and stride); any other overlap is undefined,
+ *   and two outputs never overlap.
+ * Arithmetic is float32; a bfloat16 result is rounded to nearest even once,
+ *   when it is stored.  A call with R = 0 changes nothing but the sums over
+ *   rows (grad_weight, grad_bias), which become 0.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int64_t rows;         /* R, 0 <= R < 2^31 */
+  int64_t cols;         /* C, 1 <= C <= 2^30 */
+  int32_t dtype;        /* pss_dtype of every row argument */
+  int32_t weight_dtype; /* pss_dtype of weight and bias (layer norm) */
+} pss_rows_params;
+
+/* A dropout mask, which is never stored: the forward and the backward pass
+ * make it again from these values.  Element (r, c) takes the 16-bit number
+ * u = c mod 8 (low half of word u / 2 first, then its high half) of the
+ * generator Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", SC 2011) with key (seed mod 2^32, seed / 2^32)
+ * at counter (c / 8, r, n mod 2^32, n / 2^32), n = offset + *step.  With
+ * t = floor(65536 p + 1/2) the element is dropped (0, whatever it held) when
+ * its number is below t, else multiplied by 65536 / (65536 - t): the
+ * probability is p rounded to a multiple of 2^-16, and the mean is kept for
+ * the rounded one.  The mask depends on (seed, n, r, c, p) alone, not on the
+ * strides, the type or the operator that applies it. */
+typedef struct {
+  double p;             /* probability that an element is dropped, 0 <= p <= 1 */
+  uint64_t seed;
+  uint64_t offset;      /* number of the mask: one per use of a seed */
+  const uint64_t* step; /* device memory, or NULL (0): added to offset mod 2^64
+                           when the kernel runs, so that the replays of a
+                           captured graph can have masks of their own */
+} pss_dropout_params;
+
+/* out = residual + D(x), D the dropout (residual may be NULL: out = D(x)).
+ * The gradient of x is the same call on the gradient of out, without a
+ * residual; that of the residual is the gradient of out itself. */
+int pss_dropout(const pss_rows_params* params, const pss_dropout_params* dropout, const void* x,
+                int64_t x_stride, const void* residual, int64_t residual_stride, void* out,
+                int64_t out_stride, hipStream_t stream);
+
+/* Layer norm of every row, of the sum of a residual and the dropped-out x:
+ *   s = residual + D(x)                 (residual NULL: 0; dropout NULL: D(x) = x)
+ *   mean = sum_c s / C,  rstd = 1 / sqrt(sum_c (s - mean)^2 / C + eps)
+ *   out = (s - mean) * rstd * weight + bias   (weight NULL: 1; bias NULL: 0)
+ * sum_out  row argument, or NULL: receives s (the residual stream goes on from
+ *          it, and the backward pass reads it)
+ * mean, rstd  device float32[R], or NULL: kept for the backward pass
+ * weight, bias  device, C elements of params->weight_dtype, or NULL
+ * eps      > 0, finite
+ * s is normalised as float32, before it is rounded for sum_out. */
+int pss_layer_norm_forward(const pss_rows_params* params, const pss_dropout_params* dropout,
+                           const void* x, int64_t x_stride, const void* residual,
+                           int64_t residual_stride, const void* weight, const void* bias, float eps,
+                           void* out, int64_t out_stride, void* sum_out, int64_t sum_stride,
+                           float* mean, float* rstd, hipStream_t stream);
+
+/* Backward of pss_layer_norm_forward.  s: the rows that were normalised
+ * (sum_out, or x where there was neither residual nor dropout); mean, rstd as
+ * kept by the forward; grad_out: the gradient of out; grad_sum (or NULL: 0):
+ * the gradient that reaches sum_out from elsewhere.
+ *   z = (s - mean) * rstd,  h = grad_out * weight
+ *   g = rstd * (h - sum_c(h) / C - z * sum_c(h * z) / C) + grad_sum
+ *   grad_residual = g,  grad_x = D(g)   (dropout NULL: g)
+ *   grad_weight = sum_r grad_out * z,   grad_bias = sum_r grad_out
+ * grad_x, grad_residual: row arguments; grad_weight, grad_bias: device
+ * float32[C], overwritten.  Each may be NULL if it is not wanted (one at
+ * least is not).  The sums over rows are taken in a fixed order that depends
+ * on R and C alone: bit-identical from run to run. */
+int pss_layer_norm_backward(const pss_rows_params* params, const pss_dropout_params* dropout,
+                            const void* grad_out, int64_t grad_out_stride, const void* s,
+                            int64_t s_stride, const void* weight, const float* mean,
+                            const float* rstd, const void* grad_sum, int64_t grad_sum_stride,
+                            void* grad_x, int64_t grad_x_stride, void* grad_residual,
+                            int64_t grad_residual_stride, float* grad_weight, float* grad_bias,
+                            hipStream_t stream);
+
+/* Learned relative position bias: attention scores [B][H][Q][K] plus a small
+ * table's entry for the bucket of each key's distance from its query, a
+ * weight shared by all pairs at that distance.
+ *
+ * Buckets.  With distance n = position of the query - position of the key,
+ * one side of S buckets holds borders[0 .. S), borders[0] = 0, non-decreasing:
+ *   bucket(n) = the number of j in 1 .. S-1 with borders[j] <= max(n, 0)
+ * bidirectional: S = num_buckets / 2, keys ahead of the query (n < 0) take
+ * S + bucket(-n); otherwise S = num_buckets and they take bucket(0).
+ * pss_position_buckets_init fills the borders of the usual map (Raffel et al.,
+ * "Exploring the limits of transfer learning", 2020): with e = S / 2, one
+ * bucket for each distance below e, and from e on steps of the logarithm that
+ * reach max_distance, where the last bucket would end:
+ *   borders[j] = j (j <= e),
+ *   borders[e + i] = smallest integer n with n >= e * (max_distance / e)^(i / (S - e))
+ * compared exactly (in integers).  A program may fill other borders itself. */
+#define PSS_MAX_BUCKETS 256
+typedef struct {
+  int32_t num_buckets;              /* >= 1; even when bidirectional */
+  int32_t bidirectional;            /* 0 or 1 */
+  int32_t borders[PSS_MAX_BUCKETS]; /* the first S are read */
+} pss_position_buckets;
+
+/* num_buckets: 2 (4 and even when bidirectional) to PSS_MAX_BUCKETS;
+ * max_distance > e.  Host only. */
+int pss_position_buckets_init(int32_t num_buckets, int32_t max_distance, int32_t bidirectional,
+                              pss_position_buckets* map);
+
+typedef struct {
+  int64_t batch, heads;      /* B, H >= 0, B * H < 2^31 */
+  int64_t queries, keys;     /* Q, K >= 0, Q <= 2^29, K <= 2^30 */
+  int32_t dtype;             /* pss_dtype of scores, out and grad_out */
+  int32_t table_dtype;       /* pss_dtype of table */
+  int64_t q_start;           /* position of query 0 (key k is at position k),
+                                0 <= q_start <= 2^29 */
+  int64_t in_stride[3];      /* of scores / grad_out: elements between batches,
+                                heads and queries (keys are consecutive); >= 0 */
+  int64_t out_stride[3];     /* of out: no two elements at one address */
+} pss_scores_params;
+
+/* out[b][h][i][k] = scores[b][h][i][k] + table[bucket][h], the bucket of
+ *   n = q_start + q_starts[b] + i - k.
+ * table     device, [num_buckets][H] of table_dtype
+ * scores    device, or NULL (0: the bias alone); out may be scores itself
+ *           (same address and strides), else they do not overlap
+ * q_starts  device int32[B], or NULL (0): where each sequence's queries begin,
+ *           for new tokens of sequences of different lengths; values are
+ *           clamped to [0, 2^29] */
+int pss_position_bias_forward(const pss_scores_params* params, const pss_position_buckets* map,
+                              const void* table, const int32_t* q_starts, const void* scores,
+                              void* out, hipStream_t stream);
+
+/* grad_table[j][h] = sum of grad_out[b][h][i][k] over the pairs of bucket j:
+ * device float32 [num_buckets][H], overwritten.  (The gradient of scores is
+ * grad_out itself.)  Sums are float32 in a fixed order that depends on the
+ * arguments' sizes and positions alone: bit-identical from run to run. */
+int pss_position_bias_backward(const pss_scores_params* params, const pss_position_buckets* map,
+                               const int32_t* q_starts, const void* grad_out, float* grad_table,
+                               hipStream_t stream);
+
+/* Host evaluation of the same bucket code the kernels run: out[m] = bucket of
+ * distance n = distances[m] (query position minus key position). */
+int pss_position_buckets_host(const pss_position_buckets* map, const int64_t* distances,
+                              int64_t count, int32_t* out);
+
+/* Host evaluation of the same generator code the kernels run: keep_out[r * C +
+ * c] = 1 if the mask keeps element (r, c), 0 if it drops it, for `rows` x
+ * `cols` elements from row `row0` on (dropout->step is not read: 0). */
+int pss_dropout_mask_host(const pss_dropout_params* dropout, int64_t row0, int64_t rows,
+                          int64_t cols, uint8_t* keep_out);
+
 /* Frees the scratch buffers kept between calls, the streams, events and
  * buffers of PSS_PREPARE_BACKWARD and the library's memory pools (see
  * "Memory" above), on every device that holds them, after waiting for that

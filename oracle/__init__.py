@@ -12,5 +12,7 @@ Contents
               sparse branch) and the SGD / Adagrad updates.
   brute       pure-Python loop version on tiny inputs, including the explicit
               0/1 sketch matrix S of Thm. 2 (M = S E, lookup = (S e_i)^T M).
+  rows_oracle  dropout masks, layer norm with its gradient and the relative
+              position bias with its gradient, float64.
 """
-from . import pss_oracle, brute  # noqa: F401
+from . import pss_oracle, brute, rows_oracle  # noqa: F401

@@ -7,9 +7,11 @@
 
 #include <map>
 #include <mutex>
+#include <vector>
 
 #include "../../include/pss.h"
 #include "pss_launch.hpp"
+#include "pss_rows.hpp"
 
 namespace {
 
@@ -656,6 +658,142 @@ uint64_t splitmix64_next(uint64_t* state) {
   return z ^ (z >> 31);
 }
 
+// ---------------------------------------------------------------------------
+// Operators on rows: checks shared by their entry points.
+// ---------------------------------------------------------------------------
+constexpr int64_t kMaxSpan = int64_t{1} << 48;  // elements between a first and a last row
+
+bool known_dtype(int32_t t) { return t == PSS_F32 || t == PSS_BF16; }
+
+int check_rows(const pss_rows_params* p) {
+  if (p == nullptr) return PSS_ERR_INVALID_ARG;
+  if (p->rows < 0 || p->rows > INT32_MAX) return PSS_ERR_INVALID_ARG;
+  if (p->cols < 1 || p->cols > (int64_t{1} << 30)) return PSS_ERR_INVALID_ARG;
+  return known_dtype(p->dtype) ? PSS_OK : PSS_ERR_UNSUPPORTED;
+}
+
+// A row argument that is there (R > 0): inputs may repeat rows, outputs not.
+bool rows_fit(const pss_rows_params* p, const void* ptr, int64_t stride, bool out) {
+  if (ptr == nullptr || stride < 0) return false;
+  if (p->rows <= 1) return true;
+  if (out && stride < p->cols) return false;
+  return stride <= kMaxSpan / (p->rows - 1);
+}
+bool optional_rows_fit(const pss_rows_params* p, const void* ptr, int64_t stride, bool out) {
+  return ptr == nullptr || rows_fit(p, ptr, stride, out);
+}
+
+// The mask of a call (NULL: no dropout).
+int make_drop(const pss_dropout_params* p, pss::Drop* d) {
+  *d = pss::Drop{};
+  if (p == nullptr) return PSS_OK;
+  if (!(p->p >= 0.0 && p->p <= 1.0)) return PSS_ERR_INVALID_ARG;
+  d->k0 = static_cast<uint32_t>(p->seed);
+  d->k1 = static_cast<uint32_t>(p->seed >> 32);
+  d->offset = p->offset;
+  d->step = p->step;
+  d->t = static_cast<uint32_t>(floor(65536.0 * p->p + 0.5));
+  d->scale = d->t < 65536u ? static_cast<float>(65536.0 / (65536u - d->t)) : 0.f;
+  return PSS_OK;
+}
+
+int check_map(const pss_position_buckets* m, pss::BucketMap* out) {
+  if (m == nullptr) return PSS_ERR_INVALID_ARG;
+  if (m->bidirectional != 0 && m->bidirectional != 1) return PSS_ERR_INVALID_ARG;
+  if (m->num_buckets < 1 || m->num_buckets > PSS_MAX_BUCKETS) return PSS_ERR_INVALID_ARG;
+  if (m->bidirectional && m->num_buckets % 2 != 0) return PSS_ERR_INVALID_ARG;
+  out->num = m->num_buckets;
+  out->both = m->bidirectional;
+  out->side = m->bidirectional ? m->num_buckets / 2 : m->num_buckets;
+  if (m->borders[0] != 0) return PSS_ERR_INVALID_ARG;
+  for (int i = 0; i < out->side; ++i) {
+    if (i > 0 && m->borders[i] < m->borders[i - 1]) return PSS_ERR_INVALID_ARG;
+    out->borders[i] = m->borders[i];
+  }
+  return PSS_OK;
+}
+
+// Strides of [B][H][Q] rows of K elements: within range and, for an output,
+// no two elements at one address (sorted by stride, each dimension steps over
+// everything the smaller ones reach).
+bool strides_fit(const int64_t size[3], int64_t K, const int64_t stride[3], bool out) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (stride[order[j]] > stride[order[j + 1]]) {
+        const int t = order[j];
+        order[j] = order[j + 1];
+        order[j + 1] = t;
+      }
+  int64_t reach = K;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t n = size[order[i]], s = stride[order[i]];
+    if (s < 0) return false;
+    if (n <= 1) continue;
+    if (s > kMaxSpan / (n - 1)) return false;
+    if (out && s < reach) return false;
+    reach += (n - 1) * s;
+  }
+  return true;
+}
+
+// Arguments of a bias call; kNothingToDo where there are no pairs.
+int make_bias(const pss_scores_params* p, const pss_position_buckets* map, const int32_t* q_starts,
+              pss::BiasArgs* a, pss::BucketMap* m) {
+  if (p == nullptr) return PSS_ERR_INVALID_ARG;
+  const int st = check_map(map, m);
+  if (st != PSS_OK) return st;
+  if (p->batch < 0 || p->heads < 0 || p->batch > INT32_MAX || p->heads > INT32_MAX ||
+      p->batch * p->heads > INT32_MAX)
+    return PSS_ERR_INVALID_ARG;
+  if (p->queries < 0 || p->queries > (int64_t{1} << 29)) return PSS_ERR_INVALID_ARG;
+  if (p->keys < 0 || p->keys > (int64_t{1} << 30)) return PSS_ERR_INVALID_ARG;
+  if (p->q_start < 0 || p->q_start > (int64_t{1} << 29)) return PSS_ERR_INVALID_ARG;
+  if (!known_dtype(p->dtype)) return PSS_ERR_UNSUPPORTED;
+  a->B = p->batch;
+  a->H = p->heads;
+  a->Q = p->queries;
+  a->K = p->keys;
+  a->q_start = p->q_start;
+  a->q_starts = q_starts;
+  if (a->B == 0 || a->H == 0 || a->Q == 0 || a->K == 0) return kNothingToDo;
+  const int64_t rows = a->B * a->H * a->Q;  // < 2^60
+  if (rows > kMaxSpan / a->K) return PSS_ERR_UNSUPPORTED;
+  return PSS_OK;
+}
+
+// Whether a^n >= b^(n-i) * c^i, compared exactly.
+class Natural {
+ public:
+  explicit Natural(uint32_t v) : w_{v} {}
+  void times(uint32_t f) {
+    uint64_t carry = 0;
+    for (uint32_t& x : w_) {
+      carry += static_cast<uint64_t>(x) * f;
+      x = static_cast<uint32_t>(carry);
+      carry >>= 32;
+    }
+    if (carry != 0) w_.push_back(static_cast<uint32_t>(carry));
+  }
+  bool operator<(const Natural& o) const {
+    if (w_.size() != o.w_.size()) return w_.size() < o.w_.size();
+    for (size_t i = w_.size(); i-- > 0;)
+      if (w_[i] != o.w_[i]) return w_[i] < o.w_[i];
+    return false;
+  }
+
+ private:
+  std::vector<uint32_t> w_;  // no leading zeros (factors are never 0)
+};
+bool power_reaches(uint32_t a, int n, uint32_t b, uint32_t c, int i) {
+  Natural left(1), right(1);
+  for (int k = 0; k < n; ++k) {
+    left.times(a);
+    right.times(k < i ? c : b);
+  }
+  return !(left < right);
+}
+
 }  // namespace
 
 extern "C" {
@@ -872,6 +1010,232 @@ int pss_debug_backward_route(int64_t M, int32_t Z, int32_t d, const pss_hash_par
 int pss_debug_reduce_events(void* before, void* after) {
   if ((before == nullptr) != (after == nullptr)) return PSS_ERR_INVALID_ARG;
   pss::set_reduce_events(static_cast<hipEvent_t>(before), static_cast<hipEvent_t>(after));
+  return PSS_OK;
+}
+
+int pss_dropout(const pss_rows_params* params, const pss_dropout_params* dropout, const void* x,
+                int64_t x_stride, const void* residual, int64_t residual_stride, void* out,
+                int64_t out_stride, hipStream_t stream) {
+  int st = check_rows(params);
+  if (st != PSS_OK) return st;
+  if (dropout == nullptr) return PSS_ERR_INVALID_ARG;
+  pss::Drop drop;
+  st = make_drop(dropout, &drop);
+  if (st != PSS_OK) return st;
+  if (params->rows == 0) return PSS_OK;
+  if (!rows_fit(params, x, x_stride, false) || !rows_fit(params, out, out_stride, true) ||
+      !optional_rows_fit(params, residual, residual_stride, false))
+    return PSS_ERR_INVALID_ARG;
+  return hip_status(pss::launch_dropout(params->dtype == PSS_BF16, {x, x_stride},
+                                        {residual, residual_stride}, {out, out_stride},
+                                        params->rows, params->cols, drop, stream));
+}
+
+int pss_layer_norm_forward(const pss_rows_params* params, const pss_dropout_params* dropout,
+                           const void* x, int64_t x_stride, const void* residual,
+                           int64_t residual_stride, const void* weight, const void* bias, float eps,
+                           void* out, int64_t out_stride, void* sum_out, int64_t sum_stride,
+                           float* mean, float* rstd, hipStream_t stream) {
+  int st = check_rows(params);
+  if (st != PSS_OK) return st;
+  if ((weight != nullptr || bias != nullptr) && !known_dtype(params->weight_dtype))
+    return PSS_ERR_UNSUPPORTED;
+  if (!(eps > 0.f && isfinite(eps))) return PSS_ERR_INVALID_ARG;
+  pss::Drop drop;
+  st = make_drop(dropout, &drop);
+  if (st != PSS_OK) return st;
+  if (params->rows == 0) return PSS_OK;
+  if (!rows_fit(params, x, x_stride, false) || !rows_fit(params, out, out_stride, true) ||
+      !optional_rows_fit(params, residual, residual_stride, false) ||
+      !optional_rows_fit(params, sum_out, sum_stride, true) || out == sum_out)
+    return PSS_ERR_INVALID_ARG;
+  pss::NormArgs a;
+  a.x = {x, x_stride};
+  a.residual = {residual, residual_stride};
+  a.out = {out, out_stride};
+  a.sum = {sum_out, sum_stride};
+  a.weight = weight;
+  a.bias = bias;
+  a.weight_bf16 = params->weight_dtype == PSS_BF16;
+  a.eps = eps;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.rows = params->rows;
+  a.cols = params->cols;
+  return hip_status(pss::launch_norm(params->dtype == PSS_BF16, a, drop, stream));
+}
+
+int pss_layer_norm_backward(const pss_rows_params* params, const pss_dropout_params* dropout,
+                            const void* grad_out, int64_t grad_out_stride, const void* s,
+                            int64_t s_stride, const void* weight, const float* mean,
+                            const float* rstd, const void* grad_sum, int64_t grad_sum_stride,
+                            void* grad_x, int64_t grad_x_stride, void* grad_residual,
+                            int64_t grad_residual_stride, float* grad_weight, float* grad_bias,
+                            hipStream_t stream) try {
+  int st = check_rows(params);
+  if (st != PSS_OK) return st;
+  if (weight != nullptr && !known_dtype(params->weight_dtype)) return PSS_ERR_UNSUPPORTED;
+  pss::Drop drop;
+  st = make_drop(dropout, &drop);
+  if (st != PSS_OK) return st;
+  if (params->rows == 0) {
+    hipError_t e = hipSuccess;
+    for (float* g : {grad_weight, grad_bias})
+      if (e == hipSuccess && g != nullptr) e = pss::launch_zero(g, params->cols, stream);
+    return hip_status(e);
+  }
+  if (!rows_fit(params, grad_out, grad_out_stride, false) ||
+      !rows_fit(params, s, s_stride, false) ||
+      !optional_rows_fit(params, grad_sum, grad_sum_stride, false) ||
+      !optional_rows_fit(params, grad_x, grad_x_stride, true) ||
+      !optional_rows_fit(params, grad_residual, grad_residual_stride, true) || mean == nullptr ||
+      rstd == nullptr)
+    return PSS_ERR_INVALID_ARG;
+  if (grad_x == nullptr && grad_residual == nullptr && grad_weight == nullptr &&
+      grad_bias == nullptr)
+    return PSS_ERR_INVALID_ARG;
+  if ((grad_x != nullptr && grad_x == grad_residual) ||
+      (grad_weight != nullptr && grad_weight == grad_bias))
+    return PSS_ERR_INVALID_ARG;
+  pss::NormGradArgs a;
+  a.grad = {grad_out, grad_out_stride};
+  a.s = {s, s_stride};
+  a.grad_sum = {grad_sum, grad_sum_stride};
+  a.grad_x = {grad_x, grad_x_stride};
+  a.grad_residual = {grad_residual, grad_residual_stride};
+  a.weight = weight;
+  a.weight_bf16 = params->weight_dtype == PSS_BF16;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.grad_weight = grad_weight;
+  a.grad_bias = grad_bias;
+  a.rows = params->rows;
+  a.cols = params->cols;
+  CallScratch scratch;
+  if (grad_weight != nullptr || grad_bias != nullptr) {
+    st = scratch.take(pss::norm_grad_workspace_bytes(a.rows, a.cols), stream);
+    if (st != PSS_OK) return st;
+  }
+  const hipError_t e =
+      pss::launch_norm_grad(params->dtype == PSS_BF16, a, drop, scratch.ptr(), stream);
+  const hipError_t ef = scratch.done();
+  return (e != hipSuccess || ef != hipSuccess) ? PSS_ERR_HIP : PSS_OK;
+} catch (...) {  // no host memory for the scratch's record
+  return PSS_ERR_NO_MEMORY;
+}
+
+int pss_position_buckets_init(int32_t num_buckets, int32_t max_distance, int32_t bidirectional,
+                              pss_position_buckets* map) try {
+  if (map == nullptr || (bidirectional != 0 && bidirectional != 1)) return PSS_ERR_INVALID_ARG;
+  if (num_buckets < 2 || num_buckets > PSS_MAX_BUCKETS) return PSS_ERR_INVALID_ARG;
+  if (bidirectional && (num_buckets < 4 || num_buckets % 2 != 0)) return PSS_ERR_INVALID_ARG;
+  const int32_t side = bidirectional ? num_buckets / 2 : num_buckets;
+  const int32_t e = side / 2, steps = side - e;
+  if (max_distance <= e) return PSS_ERR_INVALID_ARG;
+  pss_position_buckets m;
+  memset(&m, 0, sizeof(m));
+  m.num_buckets = num_buckets;
+  m.bidirectional = bidirectional;
+  for (int32_t j = 0; j < e; ++j) m.borders[j] = j;
+  for (int32_t i = 0; i < steps; ++i) {
+    // n >= e * (max_distance / e)^(i / steps), from a value at most a little off
+    const double ratio = static_cast<double>(max_distance) / e;
+    int64_t n = static_cast<int64_t>(e * pow(ratio, static_cast<double>(i) / steps));
+    const uint32_t D = static_cast<uint32_t>(max_distance);
+    while (n > 1 && power_reaches(static_cast<uint32_t>(n - 1), steps, e, D, i)) --n;
+    while (!power_reaches(static_cast<uint32_t>(n), steps, e, D, i)) ++n;
+    m.borders[e + i] = static_cast<int32_t>(n);
+  }
+  *map = m;
+  return PSS_OK;
+} catch (...) {  // no host memory for the comparison
+  return PSS_ERR_NO_MEMORY;
+}
+
+int pss_position_bias_forward(const pss_scores_params* params, const pss_position_buckets* map,
+                              const void* table, const int32_t* q_starts, const void* scores,
+                              void* out, hipStream_t stream) {
+  pss::BiasArgs a;
+  pss::BucketMap m;
+  const int st = make_bias(params, map, q_starts, &a, &m);
+  if (st != PSS_OK && st != kNothingToDo) return st;
+  if (!known_dtype(params->table_dtype)) return PSS_ERR_UNSUPPORTED;
+  if (st == kNothingToDo) return PSS_OK;
+  if (table == nullptr || out == nullptr) return PSS_ERR_INVALID_ARG;
+  const int64_t size[3] = {a.B, a.H, a.Q};
+  if (!strides_fit(size, a.K, params->out_stride, true) ||
+      (scores != nullptr && !strides_fit(size, a.K, params->in_stride, false)))
+    return PSS_ERR_INVALID_ARG;
+  a.table = table;
+  a.table_bf16 = params->table_dtype == PSS_BF16;
+  a.in = scores;
+  a.out = out;
+  for (int i = 0; i < 3; ++i) {
+    a.in_stride[i] = params->in_stride[i];
+    a.out_stride[i] = params->out_stride[i];
+  }
+  return hip_status(pss::launch_bias(params->dtype == PSS_BF16, a, m, stream));
+}
+
+int pss_position_bias_backward(const pss_scores_params* params, const pss_position_buckets* map,
+                               const int32_t* q_starts, const void* grad_out, float* grad_table,
+                               hipStream_t stream) try {
+  pss::BiasArgs a;
+  pss::BucketMap m;
+  int st = make_bias(params, map, q_starts, &a, &m);
+  if (st != PSS_OK && st != kNothingToDo) return st;
+  if (params->heads == 0) return PSS_OK;  // a table without entries
+  if (grad_table == nullptr) return PSS_ERR_INVALID_ARG;
+  if (st == kNothingToDo) return hip_status(pss::launch_zero(grad_table, m.num * a.H, stream));
+  const int64_t size[3] = {a.B, a.H, a.Q};
+  if (grad_out == nullptr || !strides_fit(size, a.K, params->in_stride, false))
+    return PSS_ERR_INVALID_ARG;
+  a.in = grad_out;
+  for (int i = 0; i < 3; ++i) a.in_stride[i] = params->in_stride[i];
+  if (!pss::bias_grad_fits(a, m)) return PSS_ERR_UNSUPPORTED;
+  CallScratch scratch;
+  st = scratch.take(pss::bias_grad_workspace_bytes(a, m), stream);
+  if (st != PSS_OK) return st;
+  const hipError_t e = pss::launch_bias_grad(params->dtype == PSS_BF16, a, m, scratch.ptr(),
+                                             grad_table, stream);
+  const hipError_t ef = scratch.done();
+  return (e != hipSuccess || ef != hipSuccess) ? PSS_ERR_HIP : PSS_OK;
+} catch (...) {  // no host memory for the scratch's record
+  return PSS_ERR_NO_MEMORY;
+}
+
+int pss_position_buckets_host(const pss_position_buckets* map, const int64_t* distances,
+                              int64_t count, int32_t* out) {
+  pss::BucketMap m;
+  const int st = check_map(map, &m);
+  if (st != PSS_OK) return st;
+  if (count < 0 || (count > 0 && (distances == nullptr || out == nullptr)))
+    return PSS_ERR_INVALID_ARG;
+  for (int64_t i = 0; i < count; ++i) {
+    // INT64_MIN has no negative: the far end either way
+    const int64_t n = distances[i] == INT64_MIN ? INT64_MIN + 1 : distances[i];
+    out[i] = pss::bucket_of(-n, m.borders, m.side, m.both != 0);
+  }
+  return PSS_OK;
+}
+
+int pss_dropout_mask_host(const pss_dropout_params* dropout, int64_t row0, int64_t rows,
+                          int64_t cols, uint8_t* keep_out) {
+  if (dropout == nullptr) return PSS_ERR_INVALID_ARG;
+  pss::Drop d;
+  const int st = make_drop(dropout, &d);
+  if (st != PSS_OK) return st;
+  if (row0 < 0 || rows < 0 || row0 > INT32_MAX || rows > INT32_MAX || row0 + rows > INT32_MAX)
+    return PSS_ERR_INVALID_ARG;
+  if (cols < 1 || cols > (int64_t{1} << 30) || (rows > 0 && keep_out == nullptr))
+    return PSS_ERR_INVALID_ARG;
+  for (int64_t r = 0; r < rows; ++r)
+    for (int64_t c = 0; c < cols; ++c) {
+      uint32_t w[4];
+      pss::drop_words(w, d.k0, d.k1, d.offset, static_cast<uint32_t>(c / pss::kLanePiece),
+                      static_cast<uint32_t>(row0 + r));
+      keep_out[r * cols + c] = pss::drop_number(w, static_cast<int>(c % pss::kLanePiece)) >= d.t;
+    }
   return PSS_OK;
 }
 

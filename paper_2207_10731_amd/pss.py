@@ -1,7 +1,7 @@
 """Python binding of libpss.so (ctypes): argument marshalling only.
 
-The function names are those of the C ABI.  Tensors must be contiguous and
-live on the current GPU; work is enqueued on torch's current stream unless a
+The function names are those of the C ABI.  Tensors must be contiguous (the
+operators on rows and scores: within a row) and live on the current GPU; work is enqueued on torch's current stream unless a
 stream is given.  Every computation happens in the HIP library: if it cannot
 be loaded, the first call raises.
 """
@@ -55,6 +55,49 @@ class pss_hash_params(ctypes.Structure):
     ]
 
 
+class pss_rows_params(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+    ]
+
+
+class pss_dropout_params(ctypes.Structure):
+    _fields_ = [
+        ("p", ctypes.c_double),
+        ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64),
+        ("step", ctypes.c_void_p),
+    ]
+
+
+PSS_MAX_BUCKETS = 256
+
+
+class pss_position_buckets(ctypes.Structure):
+    _fields_ = [
+        ("num_buckets", ctypes.c_int32),
+        ("bidirectional", ctypes.c_int32),
+        ("borders", ctypes.c_int32 * PSS_MAX_BUCKETS),
+    ]
+
+
+class pss_scores_params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64),
+        ("heads", ctypes.c_int64),
+        ("queries", ctypes.c_int64),
+        ("keys", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("table_dtype", ctypes.c_int32),
+        ("q_start", ctypes.c_int64),
+        ("in_stride", ctypes.c_int64 * 3),
+        ("out_stride", ctypes.c_int64 * 3),
+    ]
+
+
 _lib = None
 
 
@@ -84,12 +127,27 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pss_release_scratch.argtypes = []
     lib.pss_debug_reduce_events.argtypes = [vp, vp]
     lib.pss_debug_backward_route.argtypes = [i64, i32, i32, hp, i32, i32, vp]
+    f32 = ctypes.c_float
+    lib.pss_dropout.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    lib.pss_layer_norm_forward.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, i64,
+                                           vp, vp, vp]
+    lib.pss_layer_norm_backward.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64,
+                                            vp, i64, vp, vp, vp]
+    lib.pss_position_buckets_init.argtypes = [i32, i32, i32, vp]
+    lib.pss_position_bias_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    lib.pss_position_bias_backward.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.pss_position_buckets_host.argtypes = [vp, vp, i64, vp]
+    lib.pss_dropout_mask_host.argtypes = [vp, i64, i64, i64, vp]
     for name in ("pss_hash_params_from_seed", "pss_forward", "pss_backward_update",
                  "pss_backward_update_noalloc",
                  "pss_prepare_backward", "pss_debug_addresses", "pss_debug_signs",
                  "pss_gradient_sparse",
                  "pss_hash_bases_host", "pss_hash_signs_host", "pss_validate_offsets_host",
-                 "pss_release_scratch", "pss_debug_reduce_events", "pss_debug_backward_route"):
+                 "pss_release_scratch", "pss_debug_reduce_events", "pss_debug_backward_route",
+                 "pss_dropout", "pss_layer_norm_forward", "pss_layer_norm_backward",
+                 "pss_position_buckets_init", "pss_position_bias_forward",
+                 "pss_position_bias_backward", "pss_position_buckets_host",
+                 "pss_dropout_mask_host"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     # Return the library's runtime objects (kept scratch, prepared-grouping
@@ -473,6 +531,272 @@ def pss_debug_reduce_events(before=None, after=None):
         handles.append(ctypes.c_void_p(h))
     _check(load_library().pss_debug_reduce_events(handles[0], handles[1]),
            "pss_debug_reduce_events")
+
+
+# ---------------------------------------------------------------------------
+# Operators on rows: 2-D float32 or bfloat16 tensors whose rows are contiguous
+# (any row stride: a column range of wider rows, or an expanded input).
+# ---------------------------------------------------------------------------
+_ROW_DTYPES = {torch.float32: PSS_F32, torch.bfloat16: PSS_BF16}
+
+
+def make_dropout_params(p, seed, offset=0, step=None) -> pss_dropout_params:
+    """A dropout mask: probability ``p``, key ``seed``, number ``offset`` (both
+    taken mod 2^64).  ``step``: None, or an int64 GPU tensor of one element
+    whose value at the time the kernel runs is added to ``offset``."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must lie in [0, 1]")
+    if step is not None:
+        _need(step, torch.int64, "step")
+        _need_len(step, 1, "step")
+    params = pss_dropout_params(p, seed % 2**64, offset % 2**64,
+                                None if step is None else step.data_ptr())
+    params.step_tensor = step  # keeps its memory alive
+    return params
+
+
+def _rows_of(name, t, like, out=False):
+    """(address, stride) of a row argument of the shape, type and device of
+    `like`."""
+    if t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name} must be of shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    rows, cols = t.shape
+    stride, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"the elements of a row of {name} must be contiguous")
+    if rows < 2:
+        stride = cols
+    elif out and stride < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.data_ptr(), stride
+
+
+def _first_rows(name, t):
+    """(type, GPU) of the row argument that sets the call's shape."""
+    if t.dtype not in _ROW_DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be [rows][cols] with cols > 0, got {tuple(t.shape)}")
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensor on {t.device}, current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return _ROW_DTYPES[t.dtype], dev
+
+
+def _vector(name, t, dtype, n, dev):
+    """Address of a contiguous vector of n elements, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with {n} elements")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on GPU {dev}, not on {t.device}")
+    return t.data_ptr()
+
+
+def _drop_arg(dropout, dev):
+    if dropout is None:
+        return None
+    step = getattr(dropout, "step_tensor", None)
+    if step is not None and step.get_device() != dev:
+        raise ValueError(f"step must be on GPU {dev}, not on {step.device}")
+    return ctypes.byref(dropout)
+
+
+def pss_dropout(x, dropout, out, residual=None, stream=None):
+    """out = residual + D(x); the gradient of x is the same call on that of
+    out.  x, out, residual: [rows][cols]; ``dropout``: make_dropout_params."""
+    lib = load_library()
+    kind, dev = _first_rows("x", x)
+    if dropout is None:
+        raise ValueError("dropout is missing: make_dropout_params")
+    rows, cols = x.shape
+    xp, xs = _rows_of("x", x, x)
+    op, os_ = _rows_of("out", out, x, True)
+    rp, rs = _rows_of("residual", residual, x) if residual is not None else (None, 0)
+    _check(lib.pss_dropout(ctypes.byref(pss_rows_params(rows, cols, kind, PSS_F32)),
+                           _drop_arg(dropout, dev), xp, xs, rp, rs, op, os_,
+                           _raw_stream(stream, dev)), "pss_dropout")
+    return out
+
+
+def _norm_weights(weight, bias, cols, dev):
+    """(weight_dtype, addresses) of the learned vectors, of one type."""
+    t = weight if weight is not None else bias
+    if t is None:
+        return PSS_F32, None, None
+    if t.dtype not in _ROW_DTYPES:
+        raise TypeError(f"weight and bias must be float32 or bfloat16, got {t.dtype}")
+    return (_ROW_DTYPES[t.dtype], _vector("weight", weight, t.dtype, cols, dev),
+            _vector("bias", bias, t.dtype, cols, dev))
+
+
+def pss_layer_norm_forward(x, weight, bias, eps, out, mean=None, rstd=None, residual=None,
+                           dropout=None, sum_out=None, stream=None):
+    """out = layer norm of s = residual + D(x), row by row; sum_out receives s,
+    mean and rstd (float32 [rows]) what the backward pass needs."""
+    lib = load_library()
+    kind, dev = _first_rows("x", x)
+    rows, cols = x.shape
+    xp, xs = _rows_of("x", x, x)
+    op, os_ = _rows_of("out", out, x, True)
+    rp, rs = _rows_of("residual", residual, x) if residual is not None else (None, 0)
+    sp, ss = _rows_of("sum_out", sum_out, x, True) if sum_out is not None else (None, 0)
+    wkind, wp, bp = _norm_weights(weight, bias, cols, dev)
+    _check(lib.pss_layer_norm_forward(
+        ctypes.byref(pss_rows_params(rows, cols, kind, wkind)), _drop_arg(dropout, dev), xp, xs,
+        rp, rs, wp, bp, eps, op, os_, sp, ss, _vector("mean", mean, torch.float32, rows, dev),
+        _vector("rstd", rstd, torch.float32, rows, dev), _raw_stream(stream, dev)),
+        "pss_layer_norm_forward")
+    return out
+
+
+def pss_layer_norm_backward(grad_out, s, weight, mean, rstd, grad_x, grad_weight=None,
+                            grad_bias=None, grad_sum=None, dropout=None, grad_residual=None,
+                            stream=None):
+    """Gradients of pss_layer_norm_forward: grad_x and grad_residual (rows),
+    grad_weight and grad_bias (float32 [cols], overwritten); None where one is
+    not wanted.  s: sum_out (or x); grad_sum: the gradient that reaches sum_out
+    from elsewhere."""
+    lib = load_library()
+    kind, dev = _first_rows("grad_out", grad_out)
+    rows, cols = grad_out.shape
+    gp, gs = _rows_of("grad_out", grad_out, grad_out)
+    sp, ss = _rows_of("s", s, grad_out)
+    up, us = _rows_of("grad_sum", grad_sum, grad_out) if grad_sum is not None else (None, 0)
+    xp, xs = _rows_of("grad_x", grad_x, grad_out, True) if grad_x is not None else (None, 0)
+    rp, rs = (_rows_of("grad_residual", grad_residual, grad_out, True)
+              if grad_residual is not None else (None, 0))
+    wkind, wp, _ = _norm_weights(weight, None, cols, dev)
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd of the forward call are needed")
+    _check(lib.pss_layer_norm_backward(
+        ctypes.byref(pss_rows_params(rows, cols, kind, wkind)), _drop_arg(dropout, dev), gp, gs,
+        sp, ss, wp, _vector("mean", mean, torch.float32, rows, dev),
+        _vector("rstd", rstd, torch.float32, rows, dev), up, us, xp, xs, rp, rs,
+        _vector("grad_weight", grad_weight, torch.float32, cols, dev),
+        _vector("grad_bias", grad_bias, torch.float32, cols, dev), _raw_stream(stream, dev)),
+        "pss_layer_norm_backward")
+    return grad_x
+
+
+def make_position_buckets(num_buckets, max_distance, bidirectional) -> pss_position_buckets:
+    """The usual bucket map of relative positions (pss_position_buckets_init)."""
+    m = pss_position_buckets()
+    _check(load_library().pss_position_buckets_init(num_buckets, max_distance, int(bidirectional),
+                                                    ctypes.byref(m)), "pss_position_buckets_init")
+    return m
+
+
+_NO_STRIDES = (ctypes.c_int64 * 3)(0, 0, 0)
+
+
+def _scores_of(name, t, like):
+    """Address and strides of [B][H][Q][K] scores."""
+    if t.dim() != 4 or t.shape != like.shape:
+        raise ValueError(f"{name} must be of shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    b, h, q, one = t.stride()
+    if one != 1 and t.shape[3] > 1:
+        raise ValueError(f"the keys of {name} must be contiguous")
+    return t.data_ptr(), (ctypes.c_int64 * 3)(b, h, q)
+
+
+def _bias_sizes(name, t):
+    if t.dtype not in _ROW_DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B][H][Q][K], got {tuple(t.shape)}")
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensor on {t.device}, current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return _ROW_DTYPES[t.dtype], dev
+
+
+def _table_of(name, table, buckets, heads, dev):
+    if table.shape != (buckets.num_buckets, heads):
+        raise ValueError(f"{name} must be [{buckets.num_buckets}][{heads}], got "
+                         f"{tuple(table.shape)}")
+    return _vector(name, table, table.dtype, buckets.num_buckets * heads, dev)
+
+
+def pss_position_bias_forward(table, buckets, out, scores=None, q_start=0, q_starts=None,
+                              stream=None):
+    """out[b][h][i][k] = scores + table[bucket of query i and key k][h], query i
+    of sequence b at position q_start + q_starts[b] + i, key k at k.  out and
+    scores: [B][H][Q][K] (keys contiguous); table: [buckets][H]; q_starts:
+    int32 [B]."""
+    lib = load_library()
+    kind, dev = _bias_sizes("out", out)
+    B, H, Q, K = out.shape
+    op, ostr = _scores_of("out", out, out)
+    sp, sstr = _scores_of("scores", scores, out) if scores is not None else (None, _NO_STRIDES)
+    if table.dtype not in _ROW_DTYPES:
+        raise TypeError(f"table must be float32 or bfloat16, got {table.dtype}")
+    tp = _table_of("table", table, buckets, H, dev)
+    params = pss_scores_params(B, H, Q, K, kind, _ROW_DTYPES[table.dtype], q_start, sstr, ostr)
+    _check(lib.pss_position_bias_forward(ctypes.byref(params), ctypes.byref(buckets), tp,
+                                         _vector("q_starts", q_starts, torch.int32, B, dev), sp,
+                                         op, _raw_stream(stream, dev)),
+           "pss_position_bias_forward")
+    return out
+
+
+def pss_position_bias_backward(grad_out, buckets, grad_table, q_start=0, q_starts=None,
+                               stream=None):
+    """grad_table (float32 [buckets][H], overwritten): the sum of grad_out over
+    the pairs of each bucket.  The gradient of the scores is grad_out itself."""
+    lib = load_library()
+    kind, dev = _bias_sizes("grad_out", grad_out)
+    B, H, Q, K = grad_out.shape
+    gp, gstr = _scores_of("grad_out", grad_out, grad_out)
+    if grad_table.dtype is not torch.float32:
+        raise TypeError(f"grad_table must be {torch.float32}, got {grad_table.dtype}")
+    tp = _table_of("grad_table", grad_table, buckets, H, dev)
+    params = pss_scores_params(B, H, Q, K, kind, PSS_F32, q_start, gstr, _NO_STRIDES)
+    _check(lib.pss_position_bias_backward(ctypes.byref(params), ctypes.byref(buckets),
+                                          _vector("q_starts", q_starts, torch.int32, B, dev), gp,
+                                          tp, _raw_stream(stream, dev)),
+           "pss_position_bias_backward")
+    return grad_table
+
+
+def pss_position_buckets_host(buckets, distances):
+    """Bucket of each distance (query position minus key position): int32 array."""
+    import numpy as np
+    n = np.ascontiguousarray(distances, dtype=np.int64)
+    out = np.zeros(n.shape, dtype=np.int32)
+    _check(load_library().pss_position_buckets_host(ctypes.byref(buckets),
+                                                    n.ctypes.data_as(ctypes.c_void_p), n.size,
+                                                    out.ctypes.data_as(ctypes.c_void_p)),
+           "pss_position_buckets_host")
+    return out
+
+
+def pss_dropout_mask_host(dropout, rows, cols, row0=0):
+    """Which elements the mask keeps (uint8 [rows][cols] from row row0 on;
+    ``step`` is not read)."""
+    import numpy as np
+    out = np.zeros((max(rows, 0), max(cols, 0)), dtype=np.uint8)
+    _check(load_library().pss_dropout_mask_host(ctypes.byref(dropout), row0, rows, cols,
+                                                out.ctypes.data_as(ctypes.c_void_p)),
+           "pss_dropout_mask_host")
+    return out
 
 
 def pss_release_scratch():

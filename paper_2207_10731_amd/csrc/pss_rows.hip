@@ -6,6 +6,7 @@ namespace pss {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / kWave;
+constexpr int kNormBlocks = 256 * 8;  // blocks that walk rows: 8 to a CU
 
 // Sums of two values over the block, in every thread, in a fixed order.
 __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
@@ -141,19 +142,379 @@ __global__ __launch_bounds__(kRowThreads) void norm_wide_kernel(const NormArgs a
   }
 }
 
-hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(a.rows < 8192 ? a.rows : 8192)), block(kRowThreads);
-  if (bf16)
-    hipLaunchKernelGGL(norm_wide_kernel<uint16_t>, grid, block, 0, stream, a, drop);
-  else
-    hipLaunchKernelGGL(norm_wide_kernel<float>, grid, block, 0, stream, a, drop);
+// Rows whose elements stay in registers, by groups of G lanes of a wavefront
+// (G * NP pieces cover a row): read once, mean and squares about it from the
+// registers.  A group walks its rows with its weights in registers.
+template <typename T, int G, int NP>
+__global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs a, const Drop drop) {
+  constexpr int kRows = kRowThreads / G;
+  const int lane = threadIdx.x % G;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const float inv = 1.f / static_cast<float>(a.cols);
+  int len[NP];
+  float w[NP][kLanePiece], b[NP][kLanePiece];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
+    len[i] = piece_len(c, a.cols);
+    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+    load_weights8(b[i], a.bias, a.weight_bf16, c, len[i], 0.f);
+  }
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
+       r0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const int64_t r = r0 + threadIdx.x / G;
+    const bool mine = r < a.rows;
+    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      norm_input8<T>(v[i], a, drop, n, r, static_cast<int64_t>(i * G + lane) * kLanePiece,
+                     mine ? len[i] : 0);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
+    }
+    const float mean = group_sum<G>(sum) * inv;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) {
+        const float e = u < len[i] ? v[i][u] - mean : 0.f;
+        sq += e * e;
+      }
+    const float rstd = 1.f / sqrtf(group_sum<G>(sq) * inv + a.eps);
+    if (!mine) continue;
+    if (lane == 0) {
+      if (a.mean != nullptr) a.mean[r] = mean;
+      if (a.rstd != nullptr) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
+      if (a.sum.p != nullptr)
+        store8(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v[i], len[i]);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u)
+        v[i][u] = (v[i][u] - mean) * rstd * w[i][u] + b[i][u];
+      store8(static_cast<T*>(a.out.p) + r * a.out.stride + c, v[i], len[i]);
+    }
+  }
+}
+
+// The same by a whole block a row.  Every wavefront takes mean and squares of
+// its own part; the parts are joined through LDS with one barrier a row (the
+// squares about the common mean are those about each part's plus the part's
+// size times the square of its mean's distance).
+template <typename T, int TH, int NP>
+__global__ __launch_bounds__(TH) void norm_block_kernel(const NormArgs a, const Drop drop) {
+  constexpr int kWaves = TH / kWave;
+  __shared__ float lds[2][2 * kWaves];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const float inv = 1.f / static_cast<float>(a.cols);
+  int len[NP], count = 0;
+  float w[NP][kLanePiece], b[NP][kLanePiece];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+    len[i] = piece_len(c, a.cols);
+    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+    load_weights8(b[i], a.bias, a.weight_bf16, c, len[i], 0.f);
+  }
+  float size[kWaves];  // elements of each wavefront's part
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    int64_t e = 0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t left = a.cols - static_cast<int64_t>(i * TH + k * kWave) * kLanePiece;
+      e += left < 0 ? 0 : (left > kWave * kLanePiece ? kWave * kLanePiece : left);
+    }
+    size[k] = static_cast<float>(e);
+    if (k == wave) count = static_cast<int>(e);
+  }
+  const float inv_part = count > 0 ? 1.f / static_cast<float>(count) : 0.f;
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      norm_input8<T>(v[i], a, drop, n, r,
+                     static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece, len[i]);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
+    }
+    const float part = wave_sum(sum) * inv_part;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) {
+        const float e = u < len[i] ? v[i][u] - part : 0.f;
+        sq += e * e;
+      }
+    sq = wave_sum(sq);
+    if (lane == 0) {
+      lds[turn][wave] = part;
+      lds[turn][kWaves + wave] = sq;
+    }
+    __syncthreads();  // the other half of lds is free again at the next row's
+    float mean = 0.f, var = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) mean += size[k] * lds[turn][k];
+    mean *= inv;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const float away = lds[turn][k] - mean;
+      var += lds[turn][kWaves + k] + size[k] * (away * away);
+    }
+    const float rstd = 1.f / sqrtf(var * inv + a.eps);
+    if (threadIdx.x == 0) {
+      if (a.mean != nullptr) a.mean[r] = mean;
+      if (a.rstd != nullptr) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+      if (a.sum.p != nullptr)
+        store8(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v[i], len[i]);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u)
+        v[i][u] = (v[i][u] - mean) * rstd * w[i][u] + b[i][u];
+      store8(static_cast<T*>(a.out.p) + r * a.out.stride + c, v[i], len[i]);
+    }
+  }
+}
+
+static uint32_t row_grid(int64_t rows, int per_block, int most) {
+  const int64_t want = (rows + per_block - 1) / per_block;
+  return static_cast<uint32_t>(want < most ? want : most);
+}
+
+template <typename T, int G, int NP>
+static hipError_t launch_norm_group(const NormArgs& a, const Drop& drop, hipStream_t stream) {
+  hipLaunchKernelGGL((norm_group_kernel<T, G, NP>),
+                     dim3(row_grid(a.rows, kRowThreads / G, kNormBlocks)), dim3(kRowThreads), 0,
+                     stream, a, drop);
+  return hipGetLastError();
+}
+template <typename T, int TH, int NP>
+static hipError_t launch_norm_block(const NormArgs& a, const Drop& drop, hipStream_t stream) {
+  hipLaunchKernelGGL((norm_block_kernel<T, TH, NP>),
+                     dim3(row_grid(a.rows, 1, kNormBlocks * kRowThreads / TH)), dim3(TH), 0, stream,
+                     a, drop);
   return hipGetLastError();
 }
 
-// Backward, rows of any width: block i takes rows i, i + blocks, ... and adds
-// its part of the weight's and bias's gradients to its own row of `part`
-// ([blocks][2][cols], each element always by the same thread); sum_parts_kernel
-// then adds the blocks' parts in order.
+template <typename T>
+static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t stream) {
+  const int64_t pieces = (a.cols + kLanePiece - 1) / kLanePiece;
+  if (pieces <= 1) return launch_norm_group<T, 1, 1>(a, drop, stream);
+  if (pieces <= 2) return launch_norm_group<T, 2, 1>(a, drop, stream);
+  if (pieces <= 4) return launch_norm_group<T, 4, 1>(a, drop, stream);
+  if (pieces <= 8) return launch_norm_group<T, 8, 1>(a, drop, stream);
+  if (pieces <= 16) return launch_norm_group<T, 16, 1>(a, drop, stream);
+  if (pieces <= 32) return launch_norm_group<T, 32, 1>(a, drop, stream);
+  if (pieces <= 64) return launch_norm_group<T, 64, 1>(a, drop, stream);
+  if (pieces <= 128) return launch_norm_group<T, 64, 2>(a, drop, stream);
+  if (pieces <= 256) return launch_norm_block<T, 256, 1>(a, drop, stream);
+  if (pieces <= 512) return launch_norm_block<T, 256, 2>(a, drop, stream);
+  if (pieces <= 1024) return launch_norm_block<T, 512, 2>(a, drop, stream);
+  if (pieces <= 2048) return launch_norm_block<T, 1024, 2>(a, drop, stream);
+  hipLaunchKernelGGL(norm_wide_kernel<T>, dim3(row_grid(a.rows, 1, kNormBlocks)), dim3(kRowThreads), 0,
+                     stream, a, drop);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream) {
+  return bf16 ? launch_norm_t<uint16_t>(a, drop, stream) : launch_norm_t<float>(a, drop, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  Each block adds what its rows give to the weight's and bias's
+// gradients to its own row of `part` ([blocks][2][cols]), and
+// sum_parts_kernel adds the blocks' rows in order.
+// ---------------------------------------------------------------------------
+
+// The row's gradient from z, h = grad * weight and their means, plus what
+// reaches the sum from elsewhere; stored, dropped out for grad_x.
+template <typename T>
+__device__ __forceinline__ void store_grads8(const NormGradArgs& a, const Drop& drop, uint64_t n,
+                                             int64_t r, int64_t c, int len, float d[kLanePiece]) {
+  if (a.grad_residual.p != nullptr)
+    store8(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, len);
+  if (a.grad_x.p != nullptr) {
+    if (drop.t) drop8(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r));
+    store8(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, len);
+  }
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_rows8(const RowsIn& x, int64_t r, int64_t c, int len) {
+  return load_raw8(static_cast<const T*>(x.p) + r * x.stride + c, len);
+}
+
+// Narrow rows, by groups of G lanes as in norm_group_kernel: a lane keeps its
+// columns' weights and gradient sums in registers for all of its rows.
+template <typename T, int G, int NP>
+__global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const NormGradArgs a,
+                                                                      const Drop drop,
+                                                                      float* part) {
+  constexpr int kRows = kRowThreads / G;
+  __shared__ float lds[kRowWaves][G * NP * kLanePiece];
+  const int lane = threadIdx.x % G, wave = threadIdx.x >> 6;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const float inv = 1.f / static_cast<float>(a.cols);
+  int len[NP];
+  float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
+    len[i] = piece_len(c, a.cols);
+    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
+  }
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
+       r0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const int64_t r = r0 + threadIdx.x / G;
+    const bool mine = r < a.rows;
+    const float mean = mine ? a.mean[r] : 0.f, rstd = mine ? a.rstd[r] : 0.f;
+    float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
+      const int m = mine ? len[i] : 0;
+      widen8(dy[i], load_rows8<T>(a.grad, r, c, m));
+      widen8(z[i], load_rows8<T>(a.s, r, c, m));
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) {
+        z[i][u] = (z[i][u] - mean) * rstd;
+        const float h = dy[i][u] * w[i][u];
+        sh += h;
+        shz += h * z[i][u];
+        gw[i][u] += dy[i][u] * z[i][u];
+        gb[i][u] += dy[i][u];
+      }
+    }
+    const float m1 = group_sum<G>(sh) * inv, m2 = group_sum<G>(shz) * inv;
+    if (!mine) continue;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
+      float d[kLanePiece];
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
+      if (a.grad_sum.p != nullptr) {
+        float q[kLanePiece];
+        widen8(q, load_rows8<T>(a.grad_sum, r, c, len[i]));
+#pragma unroll
+        for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
+      }
+      store_grads8<T>(a, drop, n, r, c, len[i], d);
+    }
+  }
+  if (part == nullptr) return;
+  // the groups of a wavefront, then the wavefronts
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) {
+        float v = which ? gb[i][u] : gw[i][u];
+#pragma unroll
+        for (int m = G; m < kWave; m <<= 1) v += __shfl_xor(v, m);
+        if ((threadIdx.x & (kWave - 1)) < G) lds[wave][(i * G + lane) * kLanePiece + u] = v;
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.cols; c += kRowThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < kRowWaves; ++k) v += lds[k][c];
+      part[(static_cast<int64_t>(blockIdx.x) * 2 + which) * a.cols + c] = v;
+    }
+  }
+}
+
+// A block a row: its wavefronts' two sums are joined through LDS with one
+// barrier a row.
+template <typename T, int TH, int NP>
+__global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs a, const Drop drop,
+                                                             float* part) {
+  constexpr int kWaves = TH / kWave;
+  __shared__ float lds[2][2 * kWaves];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const float inv = 1.f / static_cast<float>(a.cols);
+  int len[NP];
+  float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+    len[i] = piece_len(c, a.cols);
+    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
+  }
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+      widen8(dy[i], load_rows8<T>(a.grad, r, c, len[i]));
+      widen8(z[i], load_rows8<T>(a.s, r, c, len[i]));
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) {
+        z[i][u] = (z[i][u] - mean) * rstd;
+        const float h = dy[i][u] * w[i][u];
+        sh += h;
+        shz += h * z[i][u];
+        gw[i][u] += dy[i][u] * z[i][u];
+        gb[i][u] += dy[i][u];
+      }
+    }
+    sh = wave_sum(sh);
+    shz = wave_sum(shz);
+    if (lane == 0) {
+      lds[turn][wave] = sh;
+      lds[turn][kWaves + wave] = shz;
+    }
+    __syncthreads();  // the other half of lds is free again at the next row's
+    float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      m1 += lds[turn][k];
+      m2 += lds[turn][kWaves + k];
+    }
+    m1 *= inv;
+    m2 *= inv;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+      float d[kLanePiece];
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
+      if (a.grad_sum.p != nullptr) {
+        float q[kLanePiece];
+        widen8(q, load_rows8<T>(a.grad_sum, r, c, len[i]));
+#pragma unroll
+        for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
+      }
+      store_grads8<T>(a, drop, n, r, c, len[i], d);
+    }
+  }
+  if (part == nullptr) return;
+  float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+    store8(mine + c, gw[i], len[i]);
+    store8(mine + a.cols + c, gb[i], len[i]);
+  }
+}
+
+// Rows of any width: a block reads its row twice (sums, result) and keeps its
+// gradient sums in its row of `part`, each element always by the same thread.
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormGradArgs a,
                                                                      const Drop drop, float* part) {
@@ -200,12 +561,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormG
 #pragma unroll
         for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
       }
-      if (a.grad_residual.p != nullptr)
-        store8(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, len);
-      if (a.grad_x.p != nullptr) {
-        if (drop.t) drop8(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r));
-        store8(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, len);
-      }
+      store_grads8<T>(a, drop, n, r, c, len, d);
       if (part != nullptr) {
 #pragma unroll
         for (int u = 0; u < kLanePiece; ++u)
@@ -219,22 +575,58 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormG
   }
 }
 
-__global__ __launch_bounds__(kRowThreads) void sum_parts_kernel(const float* part, const int blocks,
+// Sums the blocks' parts: 32 columns a block, 32 threads of partial sums each,
+// joined in order.
+constexpr int kSumCols = 32, kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* part, const int blocks,
                                                                 const int64_t cols, float* weight,
                                                                 float* bias) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
-  if (i >= 2 * cols) return;
+  constexpr int kParts = kSumThreads / kSumCols;
+  __shared__ float lds[kParts][kSumCols + 1];
+  const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + x;
+  float v = 0.f;
+  if (i < 2 * cols)
+    for (int k = y; k < blocks; k += kParts) v += part[k * 2 * cols + i];
+  lds[y][x] = v;
+  __syncthreads();
+  if (y != 0 || i >= 2 * cols) return;
   float* out = i < cols ? weight : bias;
   if (out == nullptr) return;
-  float v = 0.f;
-  for (int k = 0; k < blocks; ++k) v += part[k * 2 * cols + i];
+  v = 0.f;
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) v += lds[k][x];
   out[i < cols ? i : i - cols] = v;
 }
 
-// Blocks of the backward: at most 2 to a CU, and at most 64 MB of parts.
+// Form of the backward's rows and its blocks: 4 of 256 threads to a CU, fewer
+// where the parts would exceed 64 MB.
+struct GradForm {
+  int threads;   // of a block
+  int lanes;     // of a row (threads: a block a row)
+  int pieces;    // of a lane; 0: the wide kernel
+};
+static GradForm grad_form(int64_t cols) {
+  const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
+  if (n <= 64) {
+    int g = 1;
+    while (g < n) g *= 2;
+    return {kRowThreads, g, 1};
+  }
+  if (n <= 128) return {kRowThreads, kWave, 2};
+  if (n <= 256) return {256, 256, 1};
+  if (n <= 512) return {256, 256, 2};
+  if (n <= 1024) return {512, 512, 2};
+  if (n <= 2048) return {1024, 1024, 2};
+  return {kRowThreads, kRowThreads, 0};
+}
 static int norm_grad_blocks(int64_t rows, int64_t cols) {
+  const GradForm f = grad_form(cols);
+  const int per_block = f.threads / f.lanes;
   const int64_t most = (int64_t{1} << 23) / cols;
-  const int64_t n = rows < 512 ? rows : 512;
+  int64_t n = (rows + per_block - 1) / per_block;
+  const int64_t fill = int64_t{4} * 256 * kRowThreads / f.threads;
+  n = n < fill ? n : fill;
   return static_cast<int>(n < most ? n : (most < 1 ? 1 : most));
 }
 
@@ -242,21 +634,46 @@ size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols) {
   return static_cast<size_t>(norm_grad_blocks(rows, cols)) * 2 * cols * sizeof(float);
 }
 
+template <typename T>
+static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, int blocks,
+                               hipStream_t stream) {
+  const GradForm f = grad_form(a.cols);
+  const dim3 grid(blocks), block(f.threads);
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop, part);
+  };
+  switch (f.pieces == 0 ? 0 : f.lanes * f.pieces) {
+    case 1: return launch(norm_grad_group_kernel<T, 1, 1>);
+    case 2: return launch(norm_grad_group_kernel<T, 2, 1>);
+    case 4: return launch(norm_grad_group_kernel<T, 4, 1>);
+    case 8: return launch(norm_grad_group_kernel<T, 8, 1>);
+    case 16: return launch(norm_grad_group_kernel<T, 16, 1>);
+    case 32: return launch(norm_grad_group_kernel<T, 32, 1>);
+    case 64: return launch(norm_grad_group_kernel<T, 64, 1>);
+    case 128: return launch(norm_grad_group_kernel<T, 64, 2>);
+    case 256: return launch(norm_grad_block_kernel<T, 256, 1>);
+    case 512: return launch(norm_grad_block_kernel<T, 256, 2>);
+    case 1024: return launch(norm_grad_block_kernel<T, 512, 2>);
+    case 2048: return launch(norm_grad_block_kernel<T, 1024, 2>);
+    default: return launch(norm_grad_wide_kernel<T>);
+  }
+}
+
 hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, void* workspace,
                             hipStream_t stream) {
   const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
   const int blocks = norm_grad_blocks(a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;
-  const dim3 grid(blocks), block(kRowThreads);
   if (bf16)
-    hipLaunchKernelGGL(norm_grad_wide_kernel<uint16_t>, grid, block, 0, stream, a, drop, part);
+    launch_norm_grad_t<uint16_t>(a, drop, part, blocks, stream);
   else
-    hipLaunchKernelGGL(norm_grad_wide_kernel<float>, grid, block, 0, stream, a, drop, part);
+    launch_norm_grad_t<float>(a, drop, part, blocks, stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums) {
     hipLaunchKernelGGL(sum_parts_kernel,
-                       dim3(static_cast<uint32_t>((2 * a.cols + kRowThreads - 1) / kRowThreads)),
-                       block, 0, stream, part, blocks, a.cols, a.grad_weight, a.grad_bias);
+                       dim3(static_cast<uint32_t>((2 * a.cols + kSumCols - 1) / kSumCols)),
+                       dim3(kSumThreads), 0, stream, part, blocks, a.cols, a.grad_weight,
+                       a.grad_bias);
     e = hipGetLastError();
   }
   return e;

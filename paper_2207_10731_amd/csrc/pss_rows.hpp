@@ -133,36 +133,72 @@ __device__ __forceinline__ void drop8(float v[kLanePiece], const Drop& d, uint64
   for (int u = 0; u < kLanePiece; ++u) v[u] = drop_number(w, u) < d.t ? 0.f : v[u] * d.scale;
 }
 
+// Pieces in memory: 16-byte loads and stores at any element (the memory system
+// takes them at any alignment of whole elements).
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t h8_any __attribute__((ext_vector_type(8), aligned(2)));
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+  f4_any a, b;
+};
+template <>
+struct Raw8<uint16_t> {
+  h8_any a;
+};
 
-// n (1 .. 8) elements from p on; the others of the piece are 0.  Whole pieces
-// take 16-byte loads whatever their alignment: the memory system takes those
-// at any element.
-__device__ __forceinline__ void load8(float v[kLanePiece], const float* p, int n) {
+// n elements from p on (8 or more: a whole piece); the others are 0.
+__device__ __forceinline__ Raw8<float> load_raw8(const float* p, int n) {
+  Raw8<float> x;
   if (n >= kLanePiece) {
-    const f4_any a = *reinterpret_cast<const f4_any*>(p);
-    const f4_any b = *reinterpret_cast<const f4_any*>(p + 4);
+    x.a = *reinterpret_cast<const f4_any*>(p);
+    x.b = *reinterpret_cast<const f4_any*>(p + 4);
+  } else {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      v[u] = a[u];
-      v[u + 4] = b[u];
+      x.a[u] = u < n ? p[u] : 0.f;
+      x.b[u] = u + 4 < n ? p[u + 4] : 0.f;
     }
-  } else {
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] = u < n ? p[u] : 0.f;
   }
+  return x;
 }
-__device__ __forceinline__ void load8(float v[kLanePiece], const uint16_t* p, int n) {
+__device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int n) {
+  Raw8<uint16_t> x;
   if (n >= kLanePiece) {
-    const h8_any a = *reinterpret_cast<const h8_any*>(p);
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] = bf16_to_f32(a[u]);
+    x.a = *reinterpret_cast<const h8_any*>(p);
   } else {
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] = u < n ? bf16_to_f32(p[u]) : 0.f;
+    for (int u = 0; u < kLanePiece; ++u) x.a[u] = u < n ? p[u] : uint16_t{0};
+  }
+  return x;
+}
+__device__ __forceinline__ void widen8(float v[kLanePiece], const Raw8<float>& x) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    v[u] = x.a[u];
+    v[u + 4] = x.b[u];
   }
 }
+__device__ __forceinline__ void widen8(float v[kLanePiece], const Raw8<uint16_t>& x) {
+#pragma unroll
+  for (int u = 0; u < kLanePiece; ++u) v[u] = bf16_to_f32(x.a[u]);
+}
+template <typename T>
+__device__ __forceinline__ void load8(float v[kLanePiece], const T* p, int n) {
+  widen8(v, load_raw8(p, n));
+}
+
+// Two floats as bfloat16 bits, to nearest even (one instruction).
+typedef float f2_v __attribute__((ext_vector_type(2)));
+typedef __bf16 b2_v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const b2_v b = __builtin_convertvector(f2_v{lo, hi}, b2_v);
+  uint32_t u;
+  __builtin_memcpy(&u, &b, 4);
+  return u;
+}
+
 __device__ __forceinline__ void store8(float* p, const float v[kLanePiece], int n) {
   if (n >= kLanePiece) {
     f4_any a, b;
@@ -180,21 +216,25 @@ __device__ __forceinline__ void store8(float* p, const float v[kLanePiece], int 
   }
 }
 __device__ __forceinline__ void store8(uint16_t* p, const float v[kLanePiece], int n) {
-  if (n >= kLanePiece) {
-    h8_any a;
+  h8_any a;
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) a[u] = f32_to_bf16_rne(v[u]);
+  for (int u = 0; u < kLanePiece; u += 2) {
+    const uint32_t w = bf16_pair(v[u], v[u + 1]);
+    a[u] = static_cast<uint16_t>(w);
+    a[u + 1] = static_cast<uint16_t>(w >> 16);
+  }
+  if (n >= kLanePiece) {
     *reinterpret_cast<h8_any*>(p) = a;
   } else {
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u)
-      if (u < n) p[u] = f32_to_bf16_rne(v[u]);
+      if (u < n) p[u] = a[u];
   }
 }
 
 // Weights (bf16: their storage) of a piece; null: `fill`.
-__device__ __forceinline__ void load_weights8(float v[kLanePiece], const void* w, bool bf16, int64_t c,
-                                              int n, float fill) {
+__device__ __forceinline__ void load_weights8(float v[kLanePiece], const void* w, bool bf16,
+                                              int64_t c, int n, float fill) {
   if (w == nullptr) {
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) v[u] = fill;
@@ -205,12 +245,25 @@ __device__ __forceinline__ void load_weights8(float v[kLanePiece], const void* w
   }
 }
 
-// Sum over the wavefront, in every lane, in a fixed order.
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) v += __shfl_xor(v, m);
+// Sum over groups of G neighbouring lanes (a power of two), the same bits in
+// every lane of a group; every lane of the wavefront takes part.  Within 16
+// lanes by data-parallel moves: halves that hold equal sums are exchanged by
+// quad permutations and mirrored rows, so that lane i adds what lane i ^ m has.
+template <int CTRL>
+__device__ __forceinline__ float add_moved(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+  if (G > 1) v = add_moved<0xb1>(v);   // quad_perm 1,0,3,2
+  if (G > 2) v = add_moved<0x4e>(v);   // quad_perm 2,3,0,1
+  if (G > 4) v = add_moved<0x141>(v);  // row_half_mirror
+  if (G > 8) v = add_moved<0x140>(v);  // row_mirror
+  if (G > 16) v += __shfl_xor(v, 16);
+  if (G > 32) v += __shfl_xor(v, 32);
   return v;
 }
+__device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
 
 // Host-side launchers.
 //

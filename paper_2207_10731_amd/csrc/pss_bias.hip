@@ -8,139 +8,328 @@ constexpr int kBiasThreads = 256;
 constexpr int kBiasWaves = kBiasThreads / kWave;
 constexpr int kMaxStart = 1 << 29;  // of q_starts
 
-// Position of query 0 of batch b.
+// Position of query 0 of batch b.  Positions stay below 3 * 2^29 and keys
+// below 2^30: differences fit 32 bits.
 __device__ __forceinline__ int32_t first_position(const BiasArgs& a, int64_t b) {
   int32_t s = a.q_starts != nullptr ? a.q_starts[b] : 0;
   s = s < 0 ? 0 : (s > kMaxStart ? kMaxStart : s);
   return static_cast<int32_t>(a.q_start) + s;
 }
 
+__device__ __forceinline__ float table_entry(const BiasArgs& a, int64_t i) {
+  return a.table_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.table)[i])
+                      : static_cast<const float*>(a.table)[i];
+}
+__device__ __forceinline__ int keys_left(int64_t k, int64_t K) {
+  return K - k < kLanePiece ? static_cast<int>(K - k) : kLanePiece;
+}
+
+// ---------------------------------------------------------------------------
+// Forward, few queries (new tokens): a lane a piece of 8 keys.  Buckets are
+// ranges of distances, so a piece whose ends share one (nearly all of a long
+// cache) needs two searches, not eight.
+// ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kBiasThreads) void bias_kernel(const BiasArgs a, const BucketMap map) {
+__global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
+                                                                const BucketMap map, const int tx,
+                                                                const uint32_t tiles) {
   __shared__ int32_t borders[kMaxBuckets];
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
-  const int64_t all = a.B * a.H * a.Q * a.K;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kBiasThreads;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBiasThreads + threadIdx.x; i < all; i += step) {
-    const int64_t row = i / a.K, k = i - row * a.K;
-    const int64_t bh = row / a.Q, q = row - bh * a.Q;
-    const int64_t b = bh / a.H, h = bh - b * a.H;
-    const int32_t rel = static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q);
-    const int j = bucket_of(rel, borders, map.side, map.both);
-    float v = a.table_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.table)[j * a.H + h])
-                           : static_cast<const float*>(a.table)[j * a.H + h];
+  const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
+  const int64_t k = (static_cast<int64_t>(blockIdx.x % tiles) * tx + x) * kLanePiece;
+  const uint32_t row = blockIdx.x / tiles * (kBiasThreads / tx) + y;
+  if (k >= a.K || row >= static_cast<uint32_t>(a.B * a.H * a.Q)) return;
+  const uint32_t bh = row / static_cast<uint32_t>(a.Q), q = row - bh * static_cast<uint32_t>(a.Q);
+  const uint32_t b = bh / static_cast<uint32_t>(a.H), h = bh - b * static_cast<uint32_t>(a.H);
+  const int len = keys_left(k, a.K);
+  float v[kLanePiece];
+  Raw8<T> raw;
+  if (a.in != nullptr)
+    raw = load_raw8(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
+                        q * a.in_stride[2] + k, len);
+  const int32_t rel = static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q);
+  const int j0 = bucket_of(rel, borders, map.side, map.both);
+  const int j1 = bucket_of(rel + kLanePiece - 1, borders, map.side, map.both);
+  // behind the query buckets fall with the key, ahead of it they rise: equal
+  // ends on one side of it hold all between
+  if (j0 == j1 && (rel >= 0 || rel + kLanePiece - 1 <= 0)) {
+    const float t = table_entry(a, j0 * a.H + h);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) v[u] = t;
+  } else {
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u)
+      v[u] = table_entry(a, bucket_of(rel + u, borders, map.side, map.both) * a.H + h);
+  }
+  if (a.in != nullptr) {
+    float s[kLanePiece];
+    widen8(s, raw);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) v[u] += s[u];
+  }
+  store8(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
+             q * a.out_stride[2] + k, v, len);
+}
+
+// ---------------------------------------------------------------------------
+// Forward, many queries.  The bias of a tile of queries and keys depends on
+// key - query alone: a block writes the table's entries for the tile's
+// differences to LDS once (tile's keys + queries of them, not keys x queries),
+// and a lane reads for 8 queries and 8 keys the 15 that they take.
+// ---------------------------------------------------------------------------
+constexpr int kStep = 8;      // queries a lane takes at a time
+constexpr int kMaxSteps = 4;
+
+template <typename T, int TX>
+__global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs a,
+                                                                 const BucketMap map,
+                                                                 const int steps,
+                                                                 const int64_t q_tiles,
+                                                                 const int64_t k_tiles) {
+  constexpr int TY = kBiasThreads / TX, kKeys = TX * kLanePiece;
+  __shared__ int32_t borders[kMaxBuckets];
+  __shared__ float column[kMaxBuckets];
+  __shared__ float window[kKeys + kMaxSteps * TY * kStep];
+  const int64_t blk = blockIdx.x;
+  const int64_t kt = blk % k_tiles, qt = blk / k_tiles % q_tiles, bh = blk / (k_tiles * q_tiles);
+  const int64_t b = bh / a.H, h = bh - b * a.H;
+  for (int i = threadIdx.x; i < map.num; i += kBiasThreads) {
+    if (i < map.side) borders[i] = map.borders[i];
+    column[i] = table_entry(a, i * a.H + h);
+  }
+  const int rows = steps * TY * kStep;  // of the tile
+  const int64_t q0 = qt * rows, k0 = kt * kKeys;
+  // difference of window[0]: the tile's first key, its last query
+  const int32_t rel0 = static_cast<int32_t>(k0 - q0 - (rows - 1)) - first_position(a, b);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kKeys + rows - 1; i += kBiasThreads)
+    window[i] = column[bucket_of(rel0 + i, borders, map.side, map.both)];
+  __syncthreads();
+  const int x = threadIdx.x % TX, y = threadIdx.x / TX;
+  const int64_t k = k0 + x * kLanePiece;
+  if (k >= a.K) return;
+  const int len = keys_left(k, a.K);
+  const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
+  T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] + k;
+  for (int s = 0; s < steps; ++s) {
+    const int row = (s * TY + y) * kStep;
+    const int64_t q = q0 + row;
+    if (q >= a.Q) return;
+    Raw8<T> raw[kStep];
     if (a.in != nullptr) {
-      float x[kLanePiece];
-      load8(x, static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
-                   q * a.in_stride[2] + k, 1);
-      v += x[0];
+#pragma unroll
+      for (int j = 0; j < kStep; ++j)
+        if (q + j < a.Q) raw[j] = load_raw8(in + (q + j) * a.in_stride[2], len);
     }
-    float y[kLanePiece] = {v};
-    store8(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] + q * a.out_stride[2] +
-               k, y, 1);
+    // bias of query q + j and key k + u: near[7 + u - j]
+    const int at = x * kLanePiece + rows - 1 - row - (kStep - 1);
+    float near[kLanePiece + kStep - 1];
+#pragma unroll
+    for (int i = 0; i < kLanePiece + kStep - 1; ++i) near[i] = window[at + i];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      if (q + j >= a.Q) break;
+      float v[kLanePiece];
+      if (a.in != nullptr) {
+        widen8(v, raw[j]);
+#pragma unroll
+        for (int u = 0; u < kLanePiece; ++u) v[u] += near[kStep - 1 + u - j];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kLanePiece; ++u) v[u] = near[kStep - 1 + u - j];
+      }
+      store8(out + (q + j) * a.out_stride[2], v, len);
+    }
+  }
+}
+
+// Lanes along the keys: as many as their pieces, 16 to a whole block.
+static int key_lanes(int64_t K) {
+  const int64_t pieces = (K + kLanePiece - 1) / kLanePiece;
+  int tx = 16;
+  while (tx < pieces && tx < kBiasThreads) tx *= 2;
+  return tx;
+}
+
+template <typename T>
+static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
+  const dim3 block(kBiasThreads);
+  const int tx = key_lanes(a.K), ty = kBiasThreads / tx;
+  const int64_t keys = static_cast<int64_t>(tx) * kLanePiece;
+  const int64_t k_tiles = (a.K + keys - 1) / keys, bh = a.B * a.H;
+  if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
+    const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
+    if (row_tiles > INT32_MAX / k_tiles) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(bias_row_kernel<T>, dim3(static_cast<uint32_t>(row_tiles * k_tiles)), block, 0,
+                       stream, a, map, tx, static_cast<uint32_t>(k_tiles));
+    return hipGetLastError();
+  }
+  // as many queries to a block as leave 8 blocks to a CU
+  int steps = kMaxSteps;
+  while (steps > 1 && bh * k_tiles * ((a.Q + ty * kStep * steps - 1) / (ty * kStep * steps)) < 2048)
+    steps /= 2;
+  const int64_t q_tiles = (a.Q + ty * kStep * steps - 1) / (ty * kStep * steps);
+  if (bh > INT32_MAX / q_tiles / k_tiles) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<uint32_t>(bh * q_tiles * k_tiles));
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, map, steps, q_tiles, k_tiles);
+    return hipGetLastError();
+  };
+  switch (tx) {
+    case 16: return launch(bias_tile_kernel<T, 16>);
+    case 32: return launch(bias_tile_kernel<T, 32>);
+    case 64: return launch(bias_tile_kernel<T, 64>);
+    case 128: return launch(bias_tile_kernel<T, 128>);
+    default: return launch(bias_tile_kernel<T, 256>);
   }
 }
 
 hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
-  const int64_t want = (a.B * a.H * a.Q * a.K + kBiasThreads - 1) / kBiasThreads;
-  const dim3 grid(static_cast<uint32_t>(want < 8192 ? want : 8192)), block(kBiasThreads);
-  if (bf16)
-    hipLaunchKernelGGL(bias_kernel<uint16_t>, grid, block, 0, stream, a, map);
-  else
-    hipLaunchKernelGGL(bias_kernel<float>, grid, block, 0, stream, a, map);
-  return hipGetLastError();
+  return bf16 ? launch_bias_t<uint16_t>(a, map, stream) : launch_bias_t<float>(a, map, stream);
 }
 
 // ---------------------------------------------------------------------------
-// The table's gradient.  All pairs at one distance share a bucket, so a block
-// first sums along diagonals: a lane owns 8 neighbouring values of
-// key - query and walks the queries of its tile, reading the 8 elements of
-// each row that lie at them.  Then every bucket, a range of distances,
-// sums its diagonals.  Every sum has a fixed order.
+// The table's gradient.  All pairs at one difference key - query share a
+// bucket, so sums are taken along diagonals first.  A group of TX lanes
+// takes TX * 8 keys and walks queries 8 at a time: a lane's 8 x 8 elements lie
+// on 15 diagonals, which it sums in registers.  After a step the 8 upper ones
+// (difference >= that of its first key and the step's first query) are done
+// for this lane and are added to the group's window in LDS, where no two
+// lanes of a step share one (lane l's are 8 l .. 8 l + 7 from the step's base);
+// the 7 lower ones go on as the upper part of the next step.  At the end every
+// bucket, a range of differences, sums its part of the windows.  Every sum has
+// a fixed order.
 // ---------------------------------------------------------------------------
-constexpr int kDiagonals = kBiasThreads * kLanePiece;  // of one block
-constexpr int kGradRows = 64;                      // queries of one block
+constexpr int kMaxGradRows = 64;  // queries of one group
 
 struct GradShape {
-  int64_t tiles;   // query tiles of one (b, h)
-  int64_t chunks;  // windows of kDiagonals diagonals of one tile
+  int tx;           // lanes of a group
+  int rows;         // queries of a group
+  int64_t k_tiles;  // of one (b, h)
+  int64_t q_tiles;  // blocks of groups along the queries of one (b, h, k tile)
 };
 static GradShape grad_shape(const BiasArgs& a) {
-  const int64_t rows = a.Q < kGradRows ? a.Q : kGradRows;
-  return {(a.Q + kGradRows - 1) / kGradRows, (a.K + rows - 1 + kDiagonals - 1) / kDiagonals};
+  GradShape s;
+  s.tx = key_lanes(a.K);
+  if (s.tx > kWave) s.tx = kWave;
+  const int groups = kBiasThreads / s.tx;
+  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece;
+  s.k_tiles = (a.K + keys - 1) / keys;
+  // long walks, as long as they leave 8 blocks to a CU
+  s.rows = kMaxGradRows;
+  while (s.rows > kStep &&
+         a.B * a.H * s.k_tiles * ((a.Q + groups * s.rows - 1) / (groups * s.rows)) < 2048)
+    s.rows /= 2;
+  s.q_tiles = (a.Q + groups * s.rows - 1) / (groups * s.rows);
+  return s;
 }
 
-// Values lo .. hi of key - query that bucket j holds (hi < lo: none).
-__device__ __forceinline__ void bucket_range(int j, const BucketMap& map, int64_t* lo, int64_t* hi) {
+// Differences key - query that bucket j holds, lo .. hi (hi < lo: none).
+__device__ __forceinline__ void bucket_range(int j, const int32_t* borders, const BucketMap& map,
+                                             int32_t* lo, int32_t* hi) {
   const bool ahead = map.both && j >= map.side;
   const int i = ahead ? j - map.side : j;
-  const int64_t n0 = map.borders[i];
-  const int64_t n1 = i + 1 < map.side ? map.borders[i + 1] : (int64_t{1} << 40);
+  const int32_t n0 = borders[i], n1 = i + 1 < map.side ? borders[i + 1] : INT32_MAX;
   if (ahead) {
     *lo = n0 < 1 ? 1 : n0;
     *hi = n1 - 1;
   } else {
     *lo = 1 - n1;
     // keys ahead of the query count as distance 0 on a single side
-    *hi = !map.both && n0 == 0 && n1 > 0 ? (int64_t{1} << 40) : -n0;
+    *hi = !map.both && n0 == 0 && n1 > 0 ? INT32_MAX : -n0;
   }
 }
 
-template <typename T>
+template <typename T, int TX>
 __global__ __launch_bounds__(kBiasThreads) void bias_grad_kernel(const BiasArgs a,
                                                                  const BucketMap map,
-                                                                 const int64_t tiles,
-                                                                 const int64_t chunks,
+                                                                 const int rows,
+                                                                 const int64_t q_tiles,
+                                                                 const int64_t k_tiles,
                                                                  float* __restrict__ part) {
-  __shared__ float diag[kDiagonals];
+  constexpr int kGroups = kBiasThreads / TX, kKeys = TX * kLanePiece;
+  constexpr int kWindow = kKeys + kMaxGradRows;
+  constexpr int kWaveGroups = kWave / TX;
+  __shared__ __align__(16) float windows[kGroups][kWindow];
+  __shared__ int32_t borders[kMaxBuckets];
+  __shared__ float sums[kBiasWaves][kMaxBuckets];
   const int64_t blk = blockIdx.x;
-  const int64_t chunk = blk % chunks, tile = blk / chunks % tiles, bh = blk / (chunks * tiles);
+  const int64_t kt = blk % k_tiles, qt = blk / k_tiles % q_tiles, bh = blk / (k_tiles * q_tiles);
   const int64_t b = bh / a.H, h = bh - b * a.H;
-  const int64_t q0 = tile * kGradRows, q1 = q0 + kGradRows < a.Q ? q0 + kGradRows : a.Q;
-  // first diagonal of the window: key 0 of the tile's last query
-  const int64_t base = -(q1 - 1) + chunk * kDiagonals;  // key index - query index
-  const int64_t mine = base + threadIdx.x * kLanePiece;
-  const T* g = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1];
-  float sum[kLanePiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int64_t q = q0; q < q1; ++q) {
-    const int64_t k = q + mine;
-    const T* p = g + q * a.in_stride[2] + k;
-    if (k >= 0 && k + kLanePiece <= a.K) {
+  const int x = threadIdx.x % TX, group = threadIdx.x / TX;
+  float* window = windows[group];
+  for (int i = x; i < kWindow; i += TX) window[i] = 0.f;
+  for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
+  __syncthreads();
+  const int64_t q0 = (qt * kGroups + group) * rows, k = kt * kKeys + x * kLanePiece;
+  const int len = keys_left(k, a.K);
+  const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
+  // diag[i]: difference (k - q) - 7 + i at the step's first query q
+  float diag[kLanePiece + kStep - 1];
+#pragma unroll
+  for (int i = 0; i < kLanePiece + kStep - 1; ++i) diag[i] = 0.f;
+  // window[0]: difference of the group's first key and its last possible query,
+  // rows - 1 after the first, and one below it for the walk's end
+  for (int s = 0; s < rows; s += kStep) {
+    const int64_t q = q0 + s;
+    Raw8<T> raw[kStep];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) raw[j] = load_raw8(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0);
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
       float v[kLanePiece];
-      load8(v, p, kLanePiece);
+      widen8(v, raw[j]);
 #pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) sum[u] += v[u];
-    } else {
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u)
-        if (k + u >= 0 && k + u < a.K) {
-          float v[kLanePiece];
-          load8(v, p + u, 1);
-          sum[u] += v[0];
-        }
+      for (int u = 0; u < kLanePiece; ++u) diag[kStep - 1 + u - j] += v[u];
     }
+    float* done = window + x * kLanePiece + rows - s;
+#pragma unroll
+    for (int i = 0; i < kLanePiece; ++i) done[i] += diag[kStep - 1 + i];
+    wave_lds_fence();  // lane x + 1 adds there at the next step
+#pragma unroll
+    for (int i = 0; i < kStep - 1; ++i) {
+      diag[kLanePiece + i] = diag[i];
+      diag[i] = 0.f;
+    }
+    diag[kStep - 1] = 0.f;
   }
 #pragma unroll
-  for (int u = 0; u < kLanePiece; ++u) diag[threadIdx.x * kLanePiece + u] = sum[u];
+  for (int i = 1; i < kLanePiece; ++i) window[x * kLanePiece + i] += diag[kStep - 1 + i];
   __syncthreads();
-  // positions: key - query = index difference - first position
-  const int64_t rel0 = base - first_position(a, b);
-  const int lane = threadIdx.x & (kWave - 1);
-  for (int j = threadIdx.x >> 6; j < map.num; j += kBiasWaves) {
-    int64_t lo, hi;
-    bucket_range(j, map, &lo, &hi);
-    lo = lo - rel0 < 0 ? 0 : lo - rel0;
-    hi = hi - rel0 >= kDiagonals ? kDiagonals - 1 : hi - rel0;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int32_t first = first_position(a, b);
+  for (int j = 0; j < map.num; ++j) {
+    int32_t lo, hi;
+    bucket_range(j, borders, map, &lo, &hi);
     float v = 0.f;
-    for (int64_t i = lo + lane; i <= hi; i += kWave) v += diag[i];
-    v = wave_sum(v);
-    // [head][batch, tile, window][bucket]
-    if (lane == 0)
-      part[((h * a.B + b) * tiles * chunks + tile * chunks + chunk) * map.num + j] = v;
+    bool any = false;
+#pragma unroll
+    for (int g = 0; g < kWaveGroups; ++g) {
+      const int at = wave * kWaveGroups + g;
+      // difference of windows[at][0], less than the largest that a window holds
+      const int64_t rel0 = kt * kKeys - ((qt * kGroups + at) * rows + rows) - first;
+      const int64_t from = lo - rel0 < 0 ? 0 : lo - rel0;
+      const int64_t to = hi - rel0 >= kKeys + rows ? kKeys + rows - 1 : hi - rel0;
+      if (from > to) continue;
+      any = true;
+      for (int i = static_cast<int>(from) + lane; i <= to; i += kWave) v += windows[at][i];
+    }
+    if (any) v = wave_sum(v);
+    if (lane == 0) sums[wave][j] = v;
+  }
+  __syncthreads();
+  // [head][bucket][batch, tile]
+  const int64_t parts = a.B * q_tiles * k_tiles;
+  for (int j = threadIdx.x; j < map.num; j += kBiasThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kBiasWaves; ++w) v += sums[w][j];
+    part[(h * map.num + j) * parts + (b * q_tiles + qt) * k_tiles + kt] = v;
   }
 }
 
+// A block an entry of the table.
 __global__ __launch_bounds__(kBiasThreads) void bias_sum_kernel(const float* __restrict__ part,
                                                                 const int64_t parts, const int num,
                                                                 const int64_t heads,
@@ -149,7 +338,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_sum_kernel(const float* __r
   const int64_t h = blockIdx.x / num;
   const int j = static_cast<int>(blockIdx.x % num);
   float v = 0.f;
-  for (int64_t i = threadIdx.x; i < parts; i += kBiasThreads) v += part[(h * parts + i) * num + j];
+  for (int64_t i = threadIdx.x; i < parts; i += kBiasThreads) v += part[blockIdx.x * parts + i];
   v = wave_sum(v);
   if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -162,30 +351,40 @@ __global__ __launch_bounds__(kBiasThreads) void bias_sum_kernel(const float* __r
 
 bool bias_grad_fits(const BiasArgs& a, const BucketMap& map) {
   const GradShape s = grad_shape(a);
-  return a.H * map.num <= INT32_MAX && a.B * a.H <= INT32_MAX / s.tiles / s.chunks;
+  return a.H * map.num <= INT32_MAX && a.B * a.H <= INT32_MAX / s.q_tiles / s.k_tiles;
 }
 
 size_t bias_grad_workspace_bytes(const BiasArgs& a, const BucketMap& map) {
   const GradShape s = grad_shape(a);
-  return static_cast<size_t>(a.B * a.H * s.tiles * s.chunks) * map.num * sizeof(float);
+  return static_cast<size_t>(a.B * a.H * s.q_tiles * s.k_tiles) * map.num * sizeof(float);
+}
+
+template <typename T>
+static void launch_bias_grad_t(const BiasArgs& a, const BucketMap& map, const GradShape& s,
+                               float* part, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(a.B * a.H * s.q_tiles * s.k_tiles)), block(kBiasThreads);
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, map, s.rows, s.q_tiles, s.k_tiles, part);
+  };
+  switch (s.tx) {
+    case 16: return launch(bias_grad_kernel<T, 16>);
+    case 32: return launch(bias_grad_kernel<T, 32>);
+    default: return launch(bias_grad_kernel<T, 64>);
+  }
 }
 
 hipError_t launch_bias_grad(bool bf16, const BiasArgs& a, const BucketMap& map, void* workspace,
                             float* grad_table, hipStream_t stream) {
   const GradShape s = grad_shape(a);
-  const int64_t blocks = a.B * a.H * s.tiles * s.chunks;
   float* part = static_cast<float*>(workspace);
-  const dim3 grid(static_cast<uint32_t>(blocks)), block(kBiasThreads);
   if (bf16)
-    hipLaunchKernelGGL(bias_grad_kernel<uint16_t>, grid, block, 0, stream, a, map, s.tiles, s.chunks,
-                       part);
+    launch_bias_grad_t<uint16_t>(a, map, s, part, stream);
   else
-    hipLaunchKernelGGL(bias_grad_kernel<float>, grid, block, 0, stream, a, map, s.tiles, s.chunks,
-                       part);
+    launch_bias_grad_t<float>(a, map, s, part, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(bias_sum_kernel, dim3(static_cast<uint32_t>(a.H * map.num)), block, 0, stream,
-                     part, a.B * s.tiles * s.chunks, map.num, a.H, grad_table);
+  hipLaunchKernelGGL(bias_sum_kernel, dim3(static_cast<uint32_t>(a.H * map.num)), dim3(kBiasThreads), 0,
+                     stream, part, a.B * s.q_tiles * s.k_tiles, map.num, a.H, grad_table);
   return hipGetLastError();
 }
 

@@ -77,9 +77,10 @@ struct BiasArgs {
 };
 
 // Bucket of a key `rel` positions ahead of its query (rel <= 0: behind it).
-PSS_HD int bucket_of(int64_t rel, const int32_t* borders, int side, bool both) {
+template <typename I>
+PSS_HD int bucket_of(I rel, const int32_t* borders, int side, bool both) {
   const bool ahead = both && rel > 0;
-  const int64_t n = rel < 0 ? -rel : (both ? rel : 0);
+  const I n = rel < 0 ? -rel : (both ? rel : 0);
   int lo = 0, hi = side - 1;  // the largest j with borders[j] <= n (borders[0] = 0)
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;

@@ -489,7 +489,7 @@ int pss_position_buckets_init(int32_t num_buckets, int32_t max_distance, int32_t
                               pss_position_buckets* map);
 
 typedef struct {
-  int64_t batch, heads;      /* B, H >= 0, B * H < 2^31 */
+  int64_t batch, heads;      /* B, H >= 0, H <= 65535, B * H < 2^31 */
   int64_t queries, keys;     /* Q, K >= 0, Q <= 2^29, K <= 2^30 */
   int32_t dtype;             /* pss_dtype of scores, out and grad_out */
   int32_t table_dtype;       /* pss_dtype of table */

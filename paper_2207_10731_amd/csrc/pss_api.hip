@@ -743,7 +743,7 @@ int make_bias(const pss_scores_params* p, const pss_position_buckets* map, const
   if (p == nullptr) return PSS_ERR_INVALID_ARG;
   const int st = check_map(map, m);
   if (st != PSS_OK) return st;
-  if (p->batch < 0 || p->heads < 0 || p->batch > INT32_MAX || p->heads > INT32_MAX ||
+  if (p->batch < 0 || p->heads < 0 || p->batch > INT32_MAX || p->heads > 0xffff ||
       p->batch * p->heads > INT32_MAX)
     return PSS_ERR_INVALID_ARG;
   if (p->queries < 0 || p->queries > (int64_t{1} << 29)) return PSS_ERR_INVALID_ARG;

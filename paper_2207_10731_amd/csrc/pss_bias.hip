@@ -191,39 +191,19 @@ hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipSt
 
 // ---------------------------------------------------------------------------
 // The table's gradient.  All pairs at one difference key - query share a
-// bucket, so sums are taken along diagonals first.  A group of TX lanes
-// takes TX * 8 keys and walks queries 8 at a time: a lane's 8 x 8 elements lie
-// on 15 diagonals, which it sums in registers.  After a step the 8 upper ones
-// (difference >= that of its first key and the step's first query) are done
-// for this lane and are added to the group's window in LDS, where no two
-// lanes of a step share one (lane l's are 8 l .. 8 l + 7 from the step's base);
-// the 7 lower ones go on as the upper part of the next step.  At the end every
-// bucket, a range of differences, sums its part of the windows.  Every sum has
-// a fixed order.
+// bucket, and all beyond the last border share one on each side: a wavefront
+// keeps one sum per difference up to that border (near) in its window in LDS
+// and the two far sums in registers, over all of its rows, whatever their
+// batch.  A lane takes 8 keys of QU queries at a time.  Blocks of elements that are
+// far are summed whole; in a near one the 8 x QU elements lie on QU + 7
+// diagonals, summed in registers first and added to the window in two parts,
+// in each of which no two lanes of a group share a difference (lane x's are 8 x .. 8 x
+// + 7, then the QU - 1 below them), one group after the other.  At the end every
+// bucket, a range of differences, sums its part of the window.  Every sum
+// has a fixed order.
 // ---------------------------------------------------------------------------
-constexpr int kMaxGradRows = 64;  // queries of one group
-
-struct GradShape {
-  int tx;           // lanes of a group
-  int rows;         // queries of a group
-  int64_t k_tiles;  // of one (b, h)
-  int64_t q_tiles;  // blocks of groups along the queries of one (b, h, k tile)
-};
-static GradShape grad_shape(const BiasArgs& a) {
-  GradShape s;
-  s.tx = key_lanes(a.K);
-  if (s.tx > kWave) s.tx = kWave;
-  const int groups = kBiasThreads / s.tx;
-  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece;
-  s.k_tiles = (a.K + keys - 1) / keys;
-  // long walks, as long as they leave 8 blocks to a CU
-  s.rows = kMaxGradRows;
-  while (s.rows > kStep &&
-         a.B * a.H * s.k_tiles * ((a.Q + groups * s.rows - 1) / (groups * s.rows)) < 2048)
-    s.rows /= 2;
-  s.q_tiles = (a.Q + groups * s.rows - 1) / (groups * s.rows);
-  return s;
-}
+constexpr int kMaxNear = 1024;        // last border of this form
+constexpr int kNearPad = 2 * kStep;   // differences a near block reaches beyond it
 
 // Differences key - query that bucket j holds, lo .. hi (hi < lo: none).
 __device__ __forceinline__ void bucket_range(int j, const int32_t* borders, const BucketMap& map,
@@ -241,8 +221,199 @@ __device__ __forceinline__ void bucket_range(int j, const int32_t* borders, cons
   }
 }
 
+
+struct NearShape {
+  int tx;           // lanes of a group: they share rows
+  int qu;           // queries of a lane's step; 8 / qu pieces of keys along them
+  int64_t q_steps;  // steps of qu queries of one sequence
+  int64_t k_steps;  // steps of keys
+  int64_t units;    // of a wavefront: a step of each of its groups
+  int blocks;       // of a head
+  int window;       // floats of a wavefront's window
+};
+static bool is_near(const BucketMap& map) { return map.borders[map.side - 1] <= kMaxNear; }
+static NearShape near_shape(const BiasArgs& a, const BucketMap& map) {
+  NearShape s;
+  const int64_t pieces = (a.K + kLanePiece - 1) / kLanePiece;
+  s.tx = 8;
+  while (s.tx < pieces && s.tx < kWave) s.tx *= 2;
+  s.qu = kStep;
+  while (s.qu > 1 && s.qu / 2 >= a.Q) s.qu /= 2;
+  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece * (kStep / s.qu);
+  const int groups = kWave / s.tx;
+  s.q_steps = (a.Q + s.qu - 1) / s.qu;
+  s.k_steps = (a.K + keys - 1) / keys;
+  s.units = (a.B * s.q_steps + groups - 1) / groups * s.k_steps;
+  // a unit a wavefront, up to 8 blocks to a CU over all heads
+  const int64_t want = (s.units + kBiasWaves - 1) / kBiasWaves;
+  const int64_t most = 2048 / a.H < 1 ? 1 : 2048 / a.H;
+  s.blocks = static_cast<int>(want < most ? want : most);
+  const int near = map.borders[map.side - 1];
+  s.window = near + kNearPad + (map.both ? near : 0) + kNearPad + 1;
+  return s;
+}
+
+template <typename T, int TX, int QU>
+__global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
+    const BiasArgs a, const BucketMap map, const uint32_t q_steps, const uint32_t k_steps,
+    const int64_t units, const int window, float* __restrict__ part) {
+  constexpr int KU = kStep / QU, kGroups = kWave / TX;
+  extern __shared__ float windows[];  // [wavefront][window]
+  __shared__ int32_t borders[kMaxBuckets];
+  __shared__ float far[2][kBiasWaves];
+  for (int i = threadIdx.x; i < kBiasWaves * window; i += kBiasThreads) windows[i] = 0.f;
+  for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
+  __syncthreads();
+  const int near = borders[map.side - 1];
+  const int ahead = map.both ? (near > 1 ? near : 1) : 0;  // differences from here on are far
+  const int zero = near + kNearPad;                        // window[zero]: difference 0
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int x = lane % TX, group = lane / TX;
+  float* mine = windows + wave * window;
+  const uint32_t h = blockIdx.y;
+  // the wavefront's units: rows of steps, each k_steps long
+  const int64_t waves = static_cast<int64_t>(gridDim.x) * kBiasWaves;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kBiasWaves + wave;
+  const int64_t each = units / waves, more = units - each * waves;
+  int64_t unit = w * each + (w < more ? w : more);
+  const int64_t end = unit + each + (w < more ? 1 : 0);
+  uint32_t row = static_cast<uint32_t>(unit / k_steps);
+  uint32_t kt = static_cast<uint32_t>(unit - static_cast<int64_t>(row) * k_steps);
+  const uint32_t rows = static_cast<uint32_t>(a.B) * q_steps;
+  float behind_sum = 0.f, ahead_sum = 0.f;
+  for (; unit < end; ++unit) {
+    const uint32_t r = row * kGroups + group;  // this group's step
+    const uint32_t b = r / q_steps;
+    const int64_t q = static_cast<int64_t>(r - b * q_steps) * QU;
+    const int left = r < rows ? (a.Q - q < QU ? static_cast<int>(a.Q - q) : QU) : 0;
+    const int64_t k0 = (static_cast<int64_t>(kt) * KU * TX + x) * kLanePiece;
+    const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
+                  q * a.in_stride[2] + k0;
+    Raw8<T> raw[KU][QU];
+#pragma unroll
+    for (int c = 0; c < KU; ++c) {
+      const int len = keys_left(k0 + c * (TX * kLanePiece), a.K);
+#pragma unroll
+      for (int j = 0; j < QU; ++j)
+        raw[c][j] = load_raw8(in + j * a.in_stride[2] + c * (TX * kLanePiece), j < left ? len : 0);
+    }
+    const int32_t pos = (left > 0 ? first_position(a, b) : 0) + static_cast<int32_t>(q);
+#pragma unroll
+    for (int c = 0; c < KU; ++c) {
+      const int32_t k = static_cast<int32_t>(k0) + c * (TX * kLanePiece);
+      // the block's differences: low .. high
+      const int32_t low = k - (pos + QU - 1), high = k + kLanePiece - 1 - pos;
+      const bool is_behind = high <= -near, is_ahead = low >= ahead;
+      const bool is_near = !is_behind && !is_ahead && left > 0 && k < a.K;
+      float diag[kLanePiece + QU - 1];  // of low + i
+#pragma unroll
+      for (int i = 0; i < kLanePiece + QU - 1; ++i) diag[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < QU; ++j) {
+        float v[kLanePiece];
+        widen8(v, raw[c][j]);
+#pragma unroll
+        for (int u = 0; u < kLanePiece; ++u) diag[QU - 1 + u - j] += v[u];
+      }
+      if (!is_near) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kLanePiece + QU - 1; ++i) sum += diag[i];
+        if (is_behind) behind_sum += sum; else ahead_sum += sum;
+      }
+      if (__any(is_near)) {
+        float* at = mine + zero + low;
+        for (int g = 0; g < kGroups; ++g) {
+          if (is_near && group == g) {
+#pragma unroll
+            for (int i = QU - 1; i < kLanePiece + QU - 1; ++i) at[i] += diag[i];
+          }
+          wave_lds_fence();
+          if (is_near && group == g) {
+#pragma unroll
+            for (int i = 0; i < QU - 1; ++i) at[i] += diag[i];
+          }
+          wave_lds_fence();
+        }
+      }
+    }
+    if (++kt == k_steps) {
+      kt = 0;
+      ++row;
+    }
+  }
+  behind_sum = wave_sum(behind_sum);
+  ahead_sum = wave_sum(ahead_sum);
+  if (lane == 0) {
+    far[0][wave] = behind_sum;
+    far[1][wave] = ahead_sum;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < window; i += kBiasThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kBiasWaves; ++k) v += windows[k * window + i];
+    windows[i] = v;
+  }
+  __syncthreads();
+  const int behind_bucket = map.side - 1;
+  const int ahead_bucket = map.both ? map.num - 1 : bucket_of(0, borders, map.side, false);
+  for (int j = wave; j < map.num; j += kBiasWaves) {
+    int32_t lo, hi;
+    bucket_range(j, borders, map, &lo, &hi);
+    lo = lo < -zero ? -zero : lo;
+    hi = hi > window - 1 - zero ? window - 1 - zero : hi;
+    float v = 0.f;
+    for (int i = lo + lane; i <= hi; i += kWave) v += windows[zero + i];
+    v = wave_sum(v);
+#pragma unroll
+    for (int k = 0; k < kBiasWaves; ++k) {
+      if (j == behind_bucket) v += far[0][k];
+      if (j == ahead_bucket) v += far[1][k];
+    }
+    // [head][bucket][block]
+    if (lane == 0) part[(static_cast<int64_t>(h) * map.num + j) * gridDim.x + blockIdx.x] = v;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The same for maps with borders farther than that.  A group of TX lanes
+// takes TX * 8 keys and walks queries 8 at a time: a lane's 8 x 8 elements lie
+// on 15 diagonals, which it sums in registers.  After a step the 8 upper ones
+// (difference >= that of its first key and the step's first query) are done
+// for this lane and are added to the group's window in LDS, where no two
+// lanes of a step share one (lane l's are 8 l .. 8 l + 7 from the step's base);
+// the 7 lower ones go on as the upper part of the next step.  At the end every
+// bucket, a range of differences, sums its part of the windows.  Every sum has
+// a fixed order.
+// ---------------------------------------------------------------------------
+constexpr int kMaxGradRows = 64;  // queries of one group
+
+struct FarShape {
+  int tx;           // lanes of a group
+  int rows;         // queries of a group
+  int64_t k_tiles;  // of one (b, h)
+  int64_t q_tiles;  // blocks of groups along the queries of one (b, h, k tile)
+};
+static FarShape far_shape(const BiasArgs& a) {
+  FarShape s;
+  s.tx = key_lanes(a.K);
+  if (s.tx > kWave) s.tx = kWave;
+  const int groups = kBiasThreads / s.tx;
+  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece;
+  s.k_tiles = (a.K + keys - 1) / keys;
+  // long walks, as long as they leave 8 blocks to a CU
+  s.rows = kMaxGradRows;
+  while (s.rows > kStep &&
+         a.B * a.H * s.k_tiles * ((a.Q + groups * s.rows - 1) / (groups * s.rows)) < 2048)
+    s.rows /= 2;
+  s.q_tiles = (a.Q + groups * s.rows - 1) / (groups * s.rows);
+  return s;
+}
+
 template <typename T, int TX>
-__global__ __launch_bounds__(kBiasThreads) void bias_grad_kernel(const BiasArgs a,
+__global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(const BiasArgs a,
                                                                  const BucketMap map,
                                                                  const int rows,
                                                                  const int64_t q_tiles,
@@ -349,42 +520,78 @@ __global__ __launch_bounds__(kBiasThreads) void bias_sum_kernel(const float* __r
   }
 }
 
+// Parts of one entry, and whether the grids hold the call.
+static int64_t grad_parts(const BiasArgs& a, const BucketMap& map) {
+  if (is_near(map)) return near_shape(a, map).blocks;
+  const FarShape s = far_shape(a);
+  return a.B * s.q_tiles * s.k_tiles;
+}
 bool bias_grad_fits(const BiasArgs& a, const BucketMap& map) {
-  const GradShape s = grad_shape(a);
-  return a.H * map.num <= INT32_MAX && a.B * a.H <= INT32_MAX / s.q_tiles / s.k_tiles;
+  if (a.H * map.num > INT32_MAX) return false;
+  if (is_near(map)) {
+    const NearShape s = near_shape(a, map);
+    return a.B <= INT32_MAX / s.q_steps;
+  }
+  const FarShape s = far_shape(a);
+  return a.B * a.H <= INT32_MAX / s.q_tiles / s.k_tiles;
 }
 
 size_t bias_grad_workspace_bytes(const BiasArgs& a, const BucketMap& map) {
-  const GradShape s = grad_shape(a);
-  return static_cast<size_t>(a.B * a.H * s.q_tiles * s.k_tiles) * map.num * sizeof(float);
+  return static_cast<size_t>(a.H * map.num * grad_parts(a, map)) * sizeof(float);
 }
 
+template <typename T, int TX>
+static void launch_near(const BiasArgs& a, const BucketMap& map, const NearShape& s, float* part,
+                        hipStream_t stream) {
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(s.blocks, static_cast<uint32_t>(a.H)), dim3(kBiasThreads),
+                       kBiasWaves * s.window * sizeof(float), stream, a, map,
+                       static_cast<uint32_t>(s.q_steps), static_cast<uint32_t>(s.k_steps), s.units,
+                       s.window, part);
+  };
+  switch (s.qu) {
+    case 1: return launch(bias_grad_near_kernel<T, TX, 1>);
+    case 2: return launch(bias_grad_near_kernel<T, TX, 2>);
+    case 4: return launch(bias_grad_near_kernel<T, TX, 4>);
+    default: return launch(bias_grad_near_kernel<T, TX, 8>);
+  }
+}
 template <typename T>
-static void launch_bias_grad_t(const BiasArgs& a, const BucketMap& map, const GradShape& s,
-                               float* part, hipStream_t stream) {
+static void launch_far(const BiasArgs& a, const BucketMap& map, const FarShape& s, float* part,
+                       hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(a.B * a.H * s.q_tiles * s.k_tiles)), block(kBiasThreads);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, map, s.rows, s.q_tiles, s.k_tiles, part);
   };
   switch (s.tx) {
-    case 16: return launch(bias_grad_kernel<T, 16>);
-    case 32: return launch(bias_grad_kernel<T, 32>);
-    default: return launch(bias_grad_kernel<T, 64>);
+    case 16: return launch(bias_grad_far_kernel<T, 16>);
+    case 32: return launch(bias_grad_far_kernel<T, 32>);
+    default: return launch(bias_grad_far_kernel<T, 64>);
+  }
+}
+template <typename T>
+static void launch_grad_t(const BiasArgs& a, const BucketMap& map, float* part, hipStream_t stream) {
+  if (!is_near(map)) return launch_far<T>(a, map, far_shape(a), part, stream);
+  const NearShape s = near_shape(a, map);
+  switch (s.tx) {
+    case 8: return launch_near<T, 8>(a, map, s, part, stream);
+    case 16: return launch_near<T, 16>(a, map, s, part, stream);
+    case 32: return launch_near<T, 32>(a, map, s, part, stream);
+    default: return launch_near<T, 64>(a, map, s, part, stream);
   }
 }
 
 hipError_t launch_bias_grad(bool bf16, const BiasArgs& a, const BucketMap& map, void* workspace,
                             float* grad_table, hipStream_t stream) {
-  const GradShape s = grad_shape(a);
   float* part = static_cast<float*>(workspace);
   if (bf16)
-    launch_bias_grad_t<uint16_t>(a, map, s, part, stream);
+    launch_grad_t<uint16_t>(a, map, part, stream);
   else
-    launch_bias_grad_t<float>(a, map, s, part, stream);
+    launch_grad_t<float>(a, map, part, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(bias_sum_kernel, dim3(static_cast<uint32_t>(a.H * map.num)), dim3(kBiasThreads), 0,
-                     stream, part, a.B * s.q_tiles * s.k_tiles, map.num, a.H, grad_table);
+                     stream, part, grad_parts(a, map), map.num, a.H, grad_table);
   return hipGetLastError();
 }
 

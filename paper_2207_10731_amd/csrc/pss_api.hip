@@ -1192,12 +1192,12 @@ int pss_position_bias_backward(const pss_scores_params* params, const pss_positi
     return PSS_ERR_INVALID_ARG;
   a.in = grad_out;
   for (int i = 0; i < 3; ++i) a.in_stride[i] = params->in_stride[i];
-  if (!pss::bias_grad_fits(a, m)) return PSS_ERR_UNSUPPORTED;
+  const bool bf16 = params->dtype == PSS_BF16;
+  if (!pss::bias_grad_fits(bf16, a, m)) return PSS_ERR_UNSUPPORTED;
   CallScratch scratch;
-  st = scratch.take(pss::bias_grad_workspace_bytes(a, m), stream);
+  st = scratch.take(pss::bias_grad_workspace_bytes(bf16, a, m), stream);
   if (st != PSS_OK) return st;
-  const hipError_t e = pss::launch_bias_grad(params->dtype == PSS_BF16, a, m, scratch.ptr(),
-                                             grad_table, stream);
+  const hipError_t e = pss::launch_bias_grad(bf16, a, m, scratch.ptr(), grad_table, stream);
   const hipError_t ef = scratch.done();
   return (e != hipSuccess || ef != hipSuccess) ? PSS_ERR_HIP : PSS_OK;
 } catch (...) {  // no host memory for the scratch's record

@@ -20,63 +20,61 @@ __device__ __forceinline__ float table_entry(const BiasArgs& a, int64_t i) {
   return a.table_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.table)[i])
                       : static_cast<const float*>(a.table)[i];
 }
-__device__ __forceinline__ int keys_left(int64_t k, int64_t K) {
-  return K - k < kLanePiece ? static_cast<int>(K - k) : kLanePiece;
-}
+// Keys from k on, as an int; a lane takes 16 bytes of them at a time (kVec).
+__device__ __forceinline__ int keys_left(int64_t k, int64_t K) { return static_cast<int>(K - k); }
 
 // ---------------------------------------------------------------------------
-// Forward, few queries (new tokens): a lane a piece of 8 keys.  Buckets are
-// ranges of distances, so a piece whose ends share one (nearly all of a long
-// cache) needs two searches, not eight.
+// Forward, few queries (new tokens): 16 bytes of keys a lane.  Buckets are
+// ranges of distances, so keys whose ends share one (nearly all of a long cache)
+// need two searches, not one each.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
                                                                 const BucketMap map, const int tx,
                                                                 const uint32_t tiles) {
+  constexpr int V = kVec<T>;
   __shared__ int32_t borders[kMaxBuckets];
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
-  const int64_t k = (static_cast<int64_t>(blockIdx.x % tiles) * tx + x) * kLanePiece;
+  const int64_t k = (static_cast<int64_t>(blockIdx.x % tiles) * tx + x) * V;
   const uint32_t row = blockIdx.x / tiles * (kBiasThreads / tx) + y;
   if (k >= a.K || row >= static_cast<uint32_t>(a.B * a.H * a.Q)) return;
   const uint32_t bh = row / static_cast<uint32_t>(a.Q), q = row - bh * static_cast<uint32_t>(a.Q);
   const uint32_t b = bh / static_cast<uint32_t>(a.H), h = bh - b * static_cast<uint32_t>(a.H);
   const int len = keys_left(k, a.K);
-  float v[kLanePiece];
-  Raw8<T> raw;
+  float v[V];
+  typename Vec<T>::type raw;
   if (a.in != nullptr)
-    raw = load_raw8(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
+    raw = load_vec(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
                         q * a.in_stride[2] + k, len);
   const int32_t rel = static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q);
   const int j0 = bucket_of(rel, borders, map.side, map.both);
-  const int j1 = bucket_of(rel + kLanePiece - 1, borders, map.side, map.both);
+  const int j1 = bucket_of(rel + V - 1, borders, map.side, map.both);
   // behind the query buckets fall with the key, ahead of it they rise: equal
   // ends on one side of it hold all between
-  if (j0 == j1 && (rel >= 0 || rel + kLanePiece - 1 <= 0)) {
+  if (j0 == j1 && (rel >= 0 || rel + V - 1 <= 0)) {
     const float t = table_entry(a, j0 * a.H + h);
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] = t;
+    for (int u = 0; u < V; ++u) v[u] = t;
   } else {
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u)
+    for (int u = 0; u < V; ++u)
       v[u] = table_entry(a, bucket_of(rel + u, borders, map.side, map.both) * a.H + h);
   }
   if (a.in != nullptr) {
-    float s[kLanePiece];
-    widen8(s, raw);
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] += s[u];
+    for (int u = 0; u < V; ++u) v[u] += widen(raw[u]);
   }
-  store8(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
-             q * a.out_stride[2] + k, v, len);
+  store_vec(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
+                q * a.out_stride[2] + k, v, len, a.stream);
 }
 
 // ---------------------------------------------------------------------------
 // Forward, many queries.  The bias of a tile of queries and keys depends on
 // key - query alone: a block writes the table's entries for the tile's
 // differences to LDS once (tile's keys + queries of them, not keys x queries),
-// and a lane reads for 8 queries and 8 keys the 15 that they take.
+// and a lane reads for 8 queries and its keys the few that they take (8 keys: 15).
 // ---------------------------------------------------------------------------
 constexpr int kStep = 8;      // queries a lane takes at a time
 constexpr int kMaxSteps = 4;
@@ -87,7 +85,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
                                                                  const int steps,
                                                                  const int64_t q_tiles,
                                                                  const int64_t k_tiles) {
-  constexpr int TY = kBiasThreads / TX, kKeys = TX * kLanePiece;
+  constexpr int V = kVec<T>, TY = kBiasThreads / TX, kKeys = TX * V;
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float column[kMaxBuckets];
   __shared__ float window[kKeys + kMaxSteps * TY * kStep];
@@ -107,7 +105,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
     window[i] = column[bucket_of(rel0 + i, borders, map.side, map.both)];
   __syncthreads();
   const int x = threadIdx.x % TX, y = threadIdx.x / TX;
-  const int64_t k = k0 + x * kLanePiece;
+  const int64_t k = k0 + x * V;
   if (k >= a.K) return;
   const int len = keys_left(k, a.K);
   const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
@@ -116,37 +114,35 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
     const int row = (s * TY + y) * kStep;
     const int64_t q = q0 + row;
     if (q >= a.Q) return;
-    Raw8<T> raw[kStep];
+    typename Vec<T>::type raw[kStep];
     if (a.in != nullptr) {
 #pragma unroll
       for (int j = 0; j < kStep; ++j)
-        if (q + j < a.Q) raw[j] = load_raw8(in + (q + j) * a.in_stride[2], len);
+        if (q + j < a.Q) raw[j] = load_vec(in + (q + j) * a.in_stride[2], len);
     }
     // bias of query q + j and key k + u: near[7 + u - j]
-    const int at = x * kLanePiece + rows - 1 - row - (kStep - 1);
-    float near[kLanePiece + kStep - 1];
+    const int at = x * V + rows - 1 - row - (kStep - 1);
+    float near[V + kStep - 1];
 #pragma unroll
-    for (int i = 0; i < kLanePiece + kStep - 1; ++i) near[i] = window[at + i];
+    for (int i = 0; i < V + kStep - 1; ++i) near[i] = window[at + i];
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       if (q + j >= a.Q) break;
-      float v[kLanePiece];
-      if (a.in != nullptr) {
-        widen8(v, raw[j]);
+      float v[V];
 #pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) v[u] += near[kStep - 1 + u - j];
-      } else {
-#pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) v[u] = near[kStep - 1 + u - j];
+      for (int u = 0; u < V; ++u) {
+        v[u] = near[kStep - 1 + u - j];
+        if (a.in != nullptr) v[u] += widen(raw[j][u]);
       }
-      store8(out + (q + j) * a.out_stride[2], v, len);
+      store_vec(out + (q + j) * a.out_stride[2], v, len, a.stream);
     }
   }
 }
 
-// Lanes along the keys: as many as their pieces, 16 to a whole block.
-static int key_lanes(int64_t K) {
-  const int64_t pieces = (K + kLanePiece - 1) / kLanePiece;
+// Lanes along the keys, `vec` keys each: as many as there are keys, 16 to a whole
+// block.
+static int key_lanes(int64_t K, int vec) {
+  const int64_t pieces = (K + vec - 1) / vec;
   int tx = 16;
   while (tx < pieces && tx < kBiasThreads) tx *= 2;
   return tx;
@@ -155,8 +151,8 @@ static int key_lanes(int64_t K) {
 template <typename T>
 static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
   const dim3 block(kBiasThreads);
-  const int tx = key_lanes(a.K), ty = kBiasThreads / tx;
-  const int64_t keys = static_cast<int64_t>(tx) * kLanePiece;
+  const int tx = key_lanes(a.K, kVec<T>), ty = kBiasThreads / tx;
+  const int64_t keys = static_cast<int64_t>(tx) * kVec<T>;
   const int64_t k_tiles = (a.K + keys - 1) / keys, bh = a.B * a.H;
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
     const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
@@ -185,7 +181,12 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
   }
 }
 
-hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
+// Results of more than this are stored past the caches.
+constexpr int64_t kStreamBytes = int64_t{32} << 20;
+
+hipError_t launch_bias(bool bf16, const BiasArgs& args, const BucketMap& map, hipStream_t stream) {
+  BiasArgs a = args;
+  a.stream = a.B * a.H * a.Q * a.K * (bf16 ? 2 : 4) > kStreamBytes;
   return bf16 ? launch_bias_t<uint16_t>(a, map, stream) : launch_bias_t<float>(a, map, stream);
 }
 
@@ -194,11 +195,11 @@ hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipSt
 // bucket, and all beyond the last border share one on each side: a wavefront
 // keeps one sum per difference up to that border (near) in its window in LDS
 // and the two far sums in registers, over all of its rows, whatever their
-// batch.  A lane takes 8 keys of QU queries at a time.  Blocks of elements that are
-// far are summed whole; in a near one the 8 x QU elements lie on QU + 7
-// diagonals, summed in registers first and added to the window in two parts,
-// in each of which no two lanes of a group share a difference (lane x's are 8 x .. 8 x
-// + 7, then the QU - 1 below them), one group after the other.  At the end every
+// batch.  A lane takes V keys (16 bytes) of QU queries at a time.  Such blocks of
+// elements that are far are summed whole; in a near one the V x QU elements lie
+// on V + QU - 1 diagonals, summed in registers first and added to the window V at
+// a time, so that no two lanes of a group share a difference (lane x's begin V x
+// above lane 0's), one group after the other.  At the end every
 // bucket, a range of differences, sums its part of the window.  Every sum
 // has a fixed order.
 // ---------------------------------------------------------------------------
@@ -222,9 +223,26 @@ __device__ __forceinline__ void bucket_range(int j, const int32_t* borders, cons
 }
 
 
+// at[i] += diag[i] (i < V + QU - 1) from lanes whose `at` are V apart, within
+// groups that take turns: from the top, V at a time, so that no two lanes add to
+// one element at once.  The wavefront's lanes take part together.
+template <int V, int N, int GROUPS>
+__device__ __forceinline__ void add_diagonals(float* at, const float diag[N], bool mine, int group) {
+  for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+    for (int top = N - 1; top >= 0; top -= V) {
+      if (mine && group == g) {
+#pragma unroll
+        for (int i = top; i > top - V && i >= 0; --i) at[i] += diag[i];
+      }
+      wave_lds_fence();
+    }
+  }
+}
+
 struct NearShape {
   int tx;           // lanes of a group: they share rows
-  int qu;           // queries of a lane's step; 8 / qu pieces of keys along them
+  int qu;           // queries of a lane's step, beside 8 / qu pieces of keys
   int64_t q_steps;  // steps of qu queries of one sequence
   int64_t k_steps;  // steps of keys
   int64_t units;    // of a wavefront: a step of each of its groups
@@ -232,14 +250,15 @@ struct NearShape {
   int window;       // floats of a wavefront's window
 };
 static bool is_near(const BucketMap& map) { return map.borders[map.side - 1] <= kMaxNear; }
-static NearShape near_shape(const BiasArgs& a, const BucketMap& map) {
+static NearShape near_shape(bool bf16, const BiasArgs& a, const BucketMap& map) {
   NearShape s;
-  const int64_t pieces = (a.K + kLanePiece - 1) / kLanePiece;
+  const int vec = bf16 ? kVec<uint16_t> : kVec<float>;
+  const int64_t pieces = (a.K + vec - 1) / vec;
   s.tx = 8;
   while (s.tx < pieces && s.tx < kWave) s.tx *= 2;
   s.qu = kStep;
   while (s.qu > 1 && s.qu / 2 >= a.Q) s.qu /= 2;
-  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece * (kStep / s.qu);
+  const int64_t keys = static_cast<int64_t>(s.tx) * vec * (kStep / s.qu);
   const int groups = kWave / s.tx;
   s.q_steps = (a.Q + s.qu - 1) / s.qu;
   s.k_steps = (a.K + keys - 1) / keys;
@@ -257,7 +276,7 @@ template <typename T, int TX, int QU>
 __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
     const BiasArgs a, const BucketMap map, const uint32_t q_steps, const uint32_t k_steps,
     const int64_t units, const int window, float* __restrict__ part) {
-  constexpr int KU = kStep / QU, kGroups = kWave / TX;
+  constexpr int V = kVec<T>, KU = kStep / QU, kGroups = kWave / TX;
   extern __shared__ float windows[];  // [wavefront][window]
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float far[2][kBiasWaves];
@@ -287,55 +306,41 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
     const uint32_t b = r / q_steps;
     const int64_t q = static_cast<int64_t>(r - b * q_steps) * QU;
     const int left = r < rows ? (a.Q - q < QU ? static_cast<int>(a.Q - q) : QU) : 0;
-    const int64_t k0 = (static_cast<int64_t>(kt) * KU * TX + x) * kLanePiece;
+    const int64_t k0 = (static_cast<int64_t>(kt) * KU * TX + x) * V;
     const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
                   q * a.in_stride[2] + k0;
-    Raw8<T> raw[KU][QU];
+    typename Vec<T>::type raw[KU][QU];
 #pragma unroll
     for (int c = 0; c < KU; ++c) {
-      const int len = keys_left(k0 + c * (TX * kLanePiece), a.K);
+      const int len = keys_left(k0 + c * (TX * V), a.K);
 #pragma unroll
       for (int j = 0; j < QU; ++j)
-        raw[c][j] = load_raw8(in + j * a.in_stride[2] + c * (TX * kLanePiece), j < left ? len : 0);
+        raw[c][j] = load_vec(in + j * a.in_stride[2] + c * (TX * V), j < left ? len : 0);
     }
     const int32_t pos = (left > 0 ? first_position(a, b) : 0) + static_cast<int32_t>(q);
 #pragma unroll
     for (int c = 0; c < KU; ++c) {
-      const int32_t k = static_cast<int32_t>(k0) + c * (TX * kLanePiece);
+      const int32_t k = static_cast<int32_t>(k0) + c * (TX * V);
       // the block's differences: low .. high
-      const int32_t low = k - (pos + QU - 1), high = k + kLanePiece - 1 - pos;
+      const int32_t low = k - (pos + QU - 1), high = k + V - 1 - pos;
       const bool is_behind = high <= -near, is_ahead = low >= ahead;
       const bool is_near = !is_behind && !is_ahead && left > 0 && k < a.K;
-      float diag[kLanePiece + QU - 1];  // of low + i
+      float diag[V + QU - 1];  // of low + i
 #pragma unroll
-      for (int i = 0; i < kLanePiece + QU - 1; ++i) diag[i] = 0.f;
+      for (int i = 0; i < V + QU - 1; ++i) diag[i] = 0.f;
 #pragma unroll
       for (int j = 0; j < QU; ++j) {
-        float v[kLanePiece];
-        widen8(v, raw[c][j]);
 #pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) diag[QU - 1 + u - j] += v[u];
+        for (int u = 0; u < V; ++u) diag[QU - 1 + u - j] += widen(raw[c][j][u]);
       }
       if (!is_near) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kLanePiece + QU - 1; ++i) sum += diag[i];
+        for (int i = 0; i < V + QU - 1; ++i) sum += diag[i];
         if (is_behind) behind_sum += sum; else ahead_sum += sum;
       }
       if (__any(is_near)) {
-        float* at = mine + zero + low;
-        for (int g = 0; g < kGroups; ++g) {
-          if (is_near && group == g) {
-#pragma unroll
-            for (int i = QU - 1; i < kLanePiece + QU - 1; ++i) at[i] += diag[i];
-          }
-          wave_lds_fence();
-          if (is_near && group == g) {
-#pragma unroll
-            for (int i = 0; i < QU - 1; ++i) at[i] += diag[i];
-          }
-          wave_lds_fence();
-        }
+        add_diagonals<V, V + QU - 1, kGroups>(mine + zero + low, diag, is_near, group);
       }
     }
     if (++kt == k_steps) {
@@ -378,17 +383,10 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// The same for maps with borders farther than that.  A group of TX lanes
-// takes TX * 8 keys and walks queries 8 at a time: a lane's 8 x 8 elements lie
-// on 15 diagonals, which it sums in registers.  After a step the 8 upper ones
-// (difference >= that of its first key and the step's first query) are done
-// for this lane and are added to the group's window in LDS, where no two
-// lanes of a step share one (lane l's are 8 l .. 8 l + 7 from the step's base);
-// the 7 lower ones go on as the upper part of the next step.  At the end every
-// bucket, a range of differences, sums its part of the windows.  Every sum has
-// a fixed order.
-// ---------------------------------------------------------------------------
-constexpr int kMaxGradRows = 64;  // queries of one group
+// The same for maps with borders farther than that: the window holds the
+// differences of one tile of keys and up to 64 queries, and every tile sums its
+// buckets (512 x 512 scores of 8 x 16 in bfloat16: 44 us, by the form above 23).
+constexpr int kMaxGradRows = 64;  // queries of one group's tile
 
 struct FarShape {
   int tx;           // lanes of a group
@@ -396,14 +394,15 @@ struct FarShape {
   int64_t k_tiles;  // of one (b, h)
   int64_t q_tiles;  // blocks of groups along the queries of one (b, h, k tile)
 };
-static FarShape far_shape(const BiasArgs& a) {
+static FarShape far_shape(bool bf16, const BiasArgs& a) {
   FarShape s;
-  s.tx = key_lanes(a.K);
+  const int vec = bf16 ? kVec<uint16_t> : kVec<float>;
+  s.tx = key_lanes(a.K, vec);
   if (s.tx > kWave) s.tx = kWave;
   const int groups = kBiasThreads / s.tx;
-  const int64_t keys = static_cast<int64_t>(s.tx) * kLanePiece;
+  const int64_t keys = static_cast<int64_t>(s.tx) * vec;
   s.k_tiles = (a.K + keys - 1) / keys;
-  // long walks, as long as they leave 8 blocks to a CU
+  // many queries, as long as they leave 8 blocks to a CU
   s.rows = kMaxGradRows;
   while (s.rows > kStep &&
          a.B * a.H * s.k_tiles * ((a.Q + groups * s.rows - 1) / (groups * s.rows)) < 2048)
@@ -413,60 +412,40 @@ static FarShape far_shape(const BiasArgs& a) {
 }
 
 template <typename T, int TX>
-__global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(const BiasArgs a,
-                                                                 const BucketMap map,
-                                                                 const int rows,
-                                                                 const int64_t q_tiles,
-                                                                 const int64_t k_tiles,
-                                                                 float* __restrict__ part) {
-  constexpr int kGroups = kBiasThreads / TX, kKeys = TX * kLanePiece;
-  constexpr int kWindow = kKeys + kMaxGradRows;
-  constexpr int kWaveGroups = kWave / TX;
-  __shared__ __align__(16) float windows[kGroups][kWindow];
+__global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(
+    const BiasArgs a, const BucketMap map, const int rows, const int64_t q_tiles,
+    const int64_t k_tiles, float* __restrict__ part) {
+  constexpr int V = kVec<T>, kGroups = kBiasThreads / TX, kKeys = TX * V;
+  constexpr int kWaveGroups = kWave / TX, kDiagonals = V + kStep - 1;
+  __shared__ float windows[kGroups][kKeys + kMaxGradRows];
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float sums[kBiasWaves][kMaxBuckets];
   const int64_t blk = blockIdx.x;
   const int64_t kt = blk % k_tiles, qt = blk / k_tiles % q_tiles, bh = blk / (k_tiles * q_tiles);
   const int64_t b = bh / a.H, h = bh - b * a.H;
   const int x = threadIdx.x % TX, group = threadIdx.x / TX;
-  float* window = windows[group];
-  for (int i = x; i < kWindow; i += TX) window[i] = 0.f;
+  for (int i = x; i < kKeys + kMaxGradRows; i += TX) windows[group][i] = 0.f;
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
-  const int64_t q0 = (qt * kGroups + group) * rows, k = kt * kKeys + x * kLanePiece;
+  const int64_t q0 = (qt * kGroups + group) * rows, k = kt * kKeys + x * V;
   const int len = keys_left(k, a.K);
   const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
-  // diag[i]: difference (k - q) - 7 + i at the step's first query q
-  float diag[kLanePiece + kStep - 1];
-#pragma unroll
-  for (int i = 0; i < kLanePiece + kStep - 1; ++i) diag[i] = 0.f;
-  // window[0]: difference of the group's first key and its last possible query,
-  // rows - 1 after the first, and one below it for the walk's end
   for (int s = 0; s < rows; s += kStep) {
     const int64_t q = q0 + s;
-    Raw8<T> raw[kStep];
+    typename Vec<T>::type raw[kStep];
 #pragma unroll
-    for (int j = 0; j < kStep; ++j) raw[j] = load_raw8(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0);
+    for (int j = 0; j < kStep; ++j)
+      raw[j] = load_vec(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0);
+    float diag[kDiagonals];  // of difference k - q - 7 + i
 #pragma unroll
-    for (int j = 0; j < kStep; ++j) {
-      float v[kLanePiece];
-      widen8(v, raw[j]);
+    for (int i = 0; i < kDiagonals; ++i) diag[i] = 0.f;
 #pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) diag[kStep - 1 + u - j] += v[u];
-    }
-    float* done = window + x * kLanePiece + rows - s;
+    for (int j = 0; j < kStep; ++j)
 #pragma unroll
-    for (int i = 0; i < kLanePiece; ++i) done[i] += diag[kStep - 1 + i];
-    wave_lds_fence();  // lane x + 1 adds there at the next step
-#pragma unroll
-    for (int i = 0; i < kStep - 1; ++i) {
-      diag[kLanePiece + i] = diag[i];
-      diag[i] = 0.f;
-    }
-    diag[kStep - 1] = 0.f;
+      for (int u = 0; u < V; ++u) diag[kStep - 1 + u - j] += widen(raw[j][u]);
+    // groups have windows of their own: no turns
+    add_diagonals<V, kDiagonals, 1>(windows[group] + x * V + rows - kStep - s, diag, true, 0);
   }
-#pragma unroll
-  for (int i = 1; i < kLanePiece; ++i) window[x * kLanePiece + i] += diag[kStep - 1 + i];
   __syncthreads();
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const int32_t first = first_position(a, b);
@@ -478,10 +457,10 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(const BiasA
 #pragma unroll
     for (int g = 0; g < kWaveGroups; ++g) {
       const int at = wave * kWaveGroups + g;
-      // difference of windows[at][0], less than the largest that a window holds
-      const int64_t rel0 = kt * kKeys - ((qt * kGroups + at) * rows + rows) - first;
+      // difference of windows[at][0]: the tile's first key, the group's last query
+      const int64_t rel0 = kt * kKeys - ((qt * kGroups + at) * rows + rows - 1) - first;
       const int64_t from = lo - rel0 < 0 ? 0 : lo - rel0;
-      const int64_t to = hi - rel0 >= kKeys + rows ? kKeys + rows - 1 : hi - rel0;
+      const int64_t to = hi - rel0 >= kKeys + rows - 1 ? kKeys + rows - 2 : hi - rel0;
       if (from > to) continue;
       any = true;
       for (int i = static_cast<int>(from) + lane; i <= to; i += kWave) v += windows[at][i];
@@ -521,23 +500,23 @@ __global__ __launch_bounds__(kBiasThreads) void bias_sum_kernel(const float* __r
 }
 
 // Parts of one entry, and whether the grids hold the call.
-static int64_t grad_parts(const BiasArgs& a, const BucketMap& map) {
-  if (is_near(map)) return near_shape(a, map).blocks;
-  const FarShape s = far_shape(a);
+static int64_t grad_parts(bool bf16, const BiasArgs& a, const BucketMap& map) {
+  if (is_near(map)) return near_shape(bf16, a, map).blocks;
+  const FarShape s = far_shape(bf16, a);
   return a.B * s.q_tiles * s.k_tiles;
 }
-bool bias_grad_fits(const BiasArgs& a, const BucketMap& map) {
+bool bias_grad_fits(bool bf16, const BiasArgs& a, const BucketMap& map) {
   if (a.H * map.num > INT32_MAX) return false;
   if (is_near(map)) {
-    const NearShape s = near_shape(a, map);
+    const NearShape s = near_shape(bf16, a, map);
     return a.B <= INT32_MAX / s.q_steps;
   }
-  const FarShape s = far_shape(a);
+  const FarShape s = far_shape(bf16, a);
   return a.B * a.H <= INT32_MAX / s.q_tiles / s.k_tiles;
 }
 
-size_t bias_grad_workspace_bytes(const BiasArgs& a, const BucketMap& map) {
-  return static_cast<size_t>(a.H * map.num * grad_parts(a, map)) * sizeof(float);
+size_t bias_grad_workspace_bytes(bool bf16, const BiasArgs& a, const BucketMap& map) {
+  return static_cast<size_t>(a.H * map.num * grad_parts(bf16, a, map)) * sizeof(float);
 }
 
 template <typename T, int TX>
@@ -571,8 +550,8 @@ static void launch_far(const BiasArgs& a, const BucketMap& map, const FarShape& 
 }
 template <typename T>
 static void launch_grad_t(const BiasArgs& a, const BucketMap& map, float* part, hipStream_t stream) {
-  if (!is_near(map)) return launch_far<T>(a, map, far_shape(a), part, stream);
-  const NearShape s = near_shape(a, map);
+  if (!is_near(map)) return launch_far<T>(a, map, far_shape(sizeof(T) == 2, a), part, stream);
+  const NearShape s = near_shape(sizeof(T) == 2, a, map);
   switch (s.tx) {
     case 8: return launch_near<T, 8>(a, map, s, part, stream);
     case 16: return launch_near<T, 16>(a, map, s, part, stream);
@@ -591,7 +570,7 @@ hipError_t launch_bias_grad(bool bf16, const BiasArgs& a, const BucketMap& map, 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(bias_sum_kernel, dim3(static_cast<uint32_t>(a.H * map.num)), dim3(kBiasThreads), 0,
-                     stream, part, grad_parts(a, map), map.num, a.H, grad_table);
+                     stream, part, grad_parts(bf16, a, map), map.num, a.H, grad_table);
   return hipGetLastError();
 }
 

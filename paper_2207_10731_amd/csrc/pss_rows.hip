@@ -27,70 +27,128 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
   }
 }
 
-__device__ __forceinline__ int piece_len(int64_t c, int64_t cols) {
-  return cols - c < kLanePiece ? static_cast<int>(cols - c) : kLanePiece;
+// Columns from c on, as an int (a span has at most 512).
+__device__ __forceinline__ int cols_left(int64_t c, int64_t cols) {
+  return cols - c > INT32_MAX ? INT32_MAX : static_cast<int>(cols - c);
+}
+
+// Lanes to a row: as many as its pieces of 8, up to a wavefront.
+static int row_lanes(int64_t cols) {
+  const int64_t pieces = (cols + kLanePiece - 1) / kLanePiece;
+  int g = 1;
+  while (g < pieces && g < kWave) g *= 2;
+  return g;
 }
 
 // ---------------------------------------------------------------------------
-// out = residual + D(x): one lane, one piece.
+// out = residual + D(x): a span of a row to a group of G lanes.
 // ---------------------------------------------------------------------------
-template <typename T>
+template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, const RowsIn residual,
                                                               const RowsOut out, const int64_t rows,
-                                                              const int64_t cols, const Drop drop) {
-  const int64_t pieces = (cols + kLanePiece - 1) / kLanePiece, all = rows * pieces;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kRowThreads;
+                                                              const int64_t cols,
+                                                              const uint32_t spans, const Drop drop,
+                                                              const bool stream) {
+  typedef Span<T, G> S;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x; i < all; i += step) {
-    const int64_t r = i / pieces, c = (i - r * pieces) * kLanePiece;
-    const int len = piece_len(c, cols);
-    float v[kLanePiece];
-    load8(v, static_cast<const T*>(x.p) + r * x.stride + c, len);
-    if (drop.t) drop8(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r));
-    if (residual.p != nullptr) {
-      float q[kLanePiece];
-      load8(q, static_cast<const T*>(residual.p) + r * residual.stride + c, len);
+  const uint32_t tile = blockIdx.x / spans, span = blockIdx.x - tile * spans;
+  const int lane = threadIdx.x % G;
+  const int64_t r = static_cast<int64_t>(tile) * (kRowThreads / G) + threadIdx.x / G;
+  const int64_t c = static_cast<int64_t>(span) * (G * kLanePiece);
+  if (r >= rows) return;
+  const int left = cols_left(c, cols);
+  S a, b;
+  a.load(static_cast<const T*>(x.p) + r * x.stride + c, lane, left);
+  if (residual.p != nullptr)
+    b.load(static_cast<const T*>(residual.p) + r * residual.stride + c, lane, left);
+  float v[kLanePiece];
+  a.widen_to(v);
+  if (drop.t) S::drop(v, drop, n, span * G, static_cast<uint32_t>(r), lane);
+  if (residual.p != nullptr) {
+    float q[kLanePiece];
+    b.widen_to(q);
 #pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) v[u] += q[u];
-    }
-    store8(static_cast<T*>(out.p) + r * out.stride + c, v, len);
+    for (int u = 0; u < kLanePiece; ++u) v[u] += q[u];
   }
+  S::store(static_cast<T*>(out.p) + r * out.stride + c, v, lane, left, stream);
 }
 
-static uint32_t piece_grid(int64_t pieces) {
-  const int64_t want = (pieces + kRowThreads - 1) / kRowThreads;
-  const int64_t cap = 256 * 32;
-  return static_cast<uint32_t>(want < 1 ? 1 : (want > cap ? cap : want));
+// Results of more than this are stored past the caches.
+constexpr int64_t kStreamBytes = int64_t{32} << 20;
+static bool streams(bool bf16, int64_t rows, int64_t cols) {
+  return rows * cols * (bf16 ? 2 : 4) > kStreamBytes;
+}
+
+template <typename T>
+static hipError_t launch_dropout_t(const RowsIn& x, const RowsIn& residual, const RowsOut& out,
+                                   int64_t rows, int64_t cols, const Drop& drop,
+                                   hipStream_t stream) {
+  const int g = row_lanes(cols);
+  const int64_t spans = (cols + g * kLanePiece - 1) / (g * kLanePiece);
+  const int64_t tiles = (rows * g + kRowThreads - 1) / kRowThreads;
+  if (tiles > INT32_MAX / spans) return hipErrorInvalidConfiguration;
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * spans)), dim3(kRowThreads), 0,
+                       stream, x, residual, out, rows, cols, static_cast<uint32_t>(spans), drop,
+                       streams(sizeof(T) == 2, rows, cols));
+    return hipGetLastError();
+  };
+  switch (g) {
+    case 1: return launch(dropout_kernel<T, 1>);
+    case 2: return launch(dropout_kernel<T, 2>);
+    case 4: return launch(dropout_kernel<T, 4>);
+    case 8: return launch(dropout_kernel<T, 8>);
+    case 16: return launch(dropout_kernel<T, 16>);
+    case 32: return launch(dropout_kernel<T, 32>);
+    default: return launch(dropout_kernel<T, 64>);
+  }
 }
 
 hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, const RowsOut& out,
                           int64_t rows, int64_t cols, const Drop& drop, hipStream_t stream) {
-  const dim3 grid(piece_grid(rows * ((cols + kLanePiece - 1) / kLanePiece))), block(kRowThreads);
-  if (bf16)
-    hipLaunchKernelGGL(dropout_kernel<uint16_t>, grid, block, 0, stream, x, residual, out, rows,
-                       cols, drop);
-  else
-    hipLaunchKernelGGL(dropout_kernel<float>, grid, block, 0, stream, x, residual, out, rows, cols,
-                       drop);
-  return hipGetLastError();
+  return bf16 ? launch_dropout_t<uint16_t>(x, residual, out, rows, cols, drop, stream)
+              : launch_dropout_t<float>(x, residual, out, rows, cols, drop, stream);
 }
 
 // ---------------------------------------------------------------------------
 // Layer norm.
 // ---------------------------------------------------------------------------
 
-// s of one piece: residual + D(x).
-template <typename T>
-__device__ __forceinline__ void norm_input8(float v[kLanePiece], const NormArgs& a, const Drop& drop,
-                                            uint64_t n, int64_t r, int64_t c, int len) {
-  load8(v, static_cast<const T*>(a.x.p) + r * a.x.stride + c, len);
-  if (drop.t) drop8(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r));
+// s of one span: residual + D(x).
+template <typename T, int G>
+__device__ __forceinline__ void norm_input(float v[kLanePiece], const NormArgs& a, const Drop& drop,
+                                           uint64_t n, int64_t r, int64_t c, int lane, int left) {
+  Span<T, G> x, q;
+  x.load(static_cast<const T*>(a.x.p) + r * a.x.stride + c, lane, left);
+  if (a.residual.p != nullptr)
+    q.load(static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, lane, left);
+  x.widen_to(v);
+  if (drop.t)
+    Span<T, G>::drop(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r),
+                     lane);
   if (a.residual.p != nullptr) {
-    float q[kLanePiece];
-    load8(q, static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, len);
+    float w[kLanePiece];
+    q.widen_to(w);
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] += q[u];
+    for (int u = 0; u < kLanePiece; ++u) v[u] += w[u];
   }
+}
+
+template <typename T, int G>
+__device__ __forceinline__ void norm_store(float v[kLanePiece], const NormArgs& a, int64_t r,
+                                           int64_t c, int lane, int left, float mean, float rstd,
+                                           const float w[kLanePiece], const float b[kLanePiece]) {
+  typedef Span<T, G> S;
+  if (a.sum.p != nullptr)
+    S::store(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v, lane, left, a.stream);
+#pragma unroll
+  for (int u = 0; u < kLanePiece; ++u) v[u] = (v[u] - mean) * rstd * w[u] + b[u];
+  S::store(static_cast<T*>(a.out.p) + r * a.out.stride + c, v, lane, left, a.stream);
+}
+
+__device__ __forceinline__ void norm_store_stats(const NormArgs& a, int64_t r, float mean, float rstd) {
+  if (a.mean != nullptr) a.mean[r] = mean;
+  if (a.rstd != nullptr) a.rstd[r] = rstd;
 }
 
 // Rows of any width: a block a row, which it reads three times (sum, squares
@@ -98,46 +156,43 @@ __device__ __forceinline__ void norm_input8(float v[kLanePiece], const NormArgs&
 // every element is read by the lane that then stores its results.
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void norm_wide_kernel(const NormArgs a, const Drop drop) {
+  constexpr int kSpan = kWave * kLanePiece;
   __shared__ float lds[2 * kRowWaves];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t first = (threadIdx.x >> 6) * kSpan, step = kRowWaves * kSpan;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const float inv = 1.f / static_cast<float>(a.cols);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     float sum = 0.f, zero = 0.f;
-    for (int64_t c = threadIdx.x * kLanePiece; c < a.cols; c += kRowThreads * kLanePiece) {
+    for (int64_t c = first; c < a.cols; c += step) {
       float v[kLanePiece];
-      norm_input8<T>(v, a, drop, n, r, c, piece_len(c, a.cols));
+      norm_input<T, kWave>(v, a, drop, n, r, c, lane, cols_left(c, a.cols));
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[u];
     }
     block_sum2(sum, zero, lds);
     const float mean = sum * inv;
     float sq = 0.f;
-    for (int64_t c = threadIdx.x * kLanePiece; c < a.cols; c += kRowThreads * kLanePiece) {
+    for (int64_t c = first; c < a.cols; c += step) {
       float v[kLanePiece];
-      const int len = piece_len(c, a.cols);
-      norm_input8<T>(v, a, drop, n, r, c, len);
+      const int left = cols_left(c, a.cols);
+      norm_input<T, kWave>(v, a, drop, n, r, c, lane, left);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
-        const float e = u < len ? v[u] - mean : 0.f;
+        const float e = Span<T, kWave>::col(lane, u) < left ? v[u] - mean : 0.f;
         sq += e * e;
       }
     }
     block_sum2(sq, zero, lds);
     const float rstd = 1.f / sqrtf(sq * inv + a.eps);
-    if (threadIdx.x == 0) {
-      if (a.mean != nullptr) a.mean[r] = mean;
-      if (a.rstd != nullptr) a.rstd[r] = rstd;
-    }
-    for (int64_t c = threadIdx.x * kLanePiece; c < a.cols; c += kRowThreads * kLanePiece) {
+    if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
+    for (int64_t c = first; c < a.cols; c += step) {
       float v[kLanePiece], w[kLanePiece], b[kLanePiece];
-      const int len = piece_len(c, a.cols);
-      norm_input8<T>(v, a, drop, n, r, c, len);
-      load_weights8(w, a.weight, a.weight_bf16, c, len, 1.f);
-      load_weights8(b, a.bias, a.weight_bf16, c, len, 0.f);
-      if (a.sum.p != nullptr) store8(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v, len);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) v[u] = (v[u] - mean) * rstd * w[u] + b[u];
-      store8(static_cast<T*>(a.out.p) + r * a.out.stride + c, v, len);
+      const int left = cols_left(c, a.cols);
+      norm_input<T, kWave>(v, a, drop, n, r, c, lane, left);
+      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      Span<T, kWave>::weights(b, a.bias, a.weight_bf16, c, lane, left, 0.f);
+      norm_store<T, kWave>(v, a, r, c, lane, left, mean, rstd, w, b);
     }
   }
 }
@@ -147,18 +202,16 @@ __global__ __launch_bounds__(kRowThreads) void norm_wide_kernel(const NormArgs a
 // registers.  A group walks its rows with its weights in registers.
 template <typename T, int G, int NP>
 __global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs a, const Drop drop) {
-  constexpr int kRows = kRowThreads / G;
+  constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
   const int lane = threadIdx.x % G;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const float inv = 1.f / static_cast<float>(a.cols);
-  int len[NP];
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
   float w[NP][kLanePiece], b[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
-    len[i] = piece_len(c, a.cols);
-    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
-    load_weights8(b[i], a.bias, a.weight_bf16, c, len[i], 0.f);
+    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
+    Span<T, G>::weights(b[i], a.bias, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 0.f);
   }
   for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
        r0 += static_cast<int64_t>(gridDim.x) * kRows) {
@@ -167,8 +220,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs 
     float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      norm_input8<T>(v[i], a, drop, n, r, static_cast<int64_t>(i * G + lane) * kLanePiece,
-                     mine ? len[i] : 0);
+      norm_input<T, G>(v[i], a, drop, n, r, i * kSpan, lane, mine ? cols - i * kSpan : 0);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
     }
@@ -177,25 +229,15 @@ __global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs 
     for (int i = 0; i < NP; ++i)
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
-        const float e = u < len[i] ? v[i][u] - mean : 0.f;
+        const float e = i * kSpan + Span<T, G>::col(lane, u) < cols ? v[i][u] - mean : 0.f;
         sq += e * e;
       }
     const float rstd = 1.f / sqrtf(group_sum<G>(sq) * inv + a.eps);
     if (!mine) continue;
-    if (lane == 0) {
-      if (a.mean != nullptr) a.mean[r] = mean;
-      if (a.rstd != nullptr) a.rstd[r] = rstd;
-    }
+    if (lane == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
-      if (a.sum.p != nullptr)
-        store8(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v[i], len[i]);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u)
-        v[i][u] = (v[i][u] - mean) * rstd * w[i][u] + b[i][u];
-      store8(static_cast<T*>(a.out.p) + r * a.out.stride + c, v[i], len[i]);
-    }
+    for (int i = 0; i < NP; ++i)
+      norm_store<T, G>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
   }
 }
 
@@ -205,40 +247,37 @@ __global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs 
 // size times the square of its mean's distance).
 template <typename T, int TH, int NP>
 __global__ __launch_bounds__(TH) void norm_block_kernel(const NormArgs a, const Drop drop) {
-  constexpr int kWaves = TH / kWave;
+  constexpr int kWaves = TH / kWave, kSpan = kWave * kLanePiece;
   __shared__ float lds[2][2 * kWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const float inv = 1.f / static_cast<float>(a.cols);
-  int len[NP], count = 0;
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
   float w[NP][kLanePiece], b[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
-    len[i] = piece_len(c, a.cols);
-    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
-    load_weights8(b[i], a.bias, a.weight_bf16, c, len[i], 0.f);
+    const int c = (i * kWaves + wave) * kSpan;
+    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c, lane, cols - c, 1.f);
+    Span<T, kWave>::weights(b[i], a.bias, a.weight_bf16, c, lane, cols - c, 0.f);
   }
-  float size[kWaves];  // elements of each wavefront's part
-#pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
-    int64_t e = 0;
+  // elements of wavefront k's part
+  const auto size = [&](int k) {
+    int e = 0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t left = a.cols - static_cast<int64_t>(i * TH + k * kWave) * kLanePiece;
-      e += left < 0 ? 0 : (left > kWave * kLanePiece ? kWave * kLanePiece : left);
+      const int left = cols - (i * kWaves + k) * kSpan;
+      e += left < 0 ? 0 : (left > kSpan ? kSpan : left);
     }
-    size[k] = static_cast<float>(e);
-    if (k == wave) count = static_cast<int>(e);
-  }
-  const float inv_part = count > 0 ? 1.f / static_cast<float>(count) : 0.f;
+    return static_cast<float>(e);
+  };
+  const float inv_part = size(wave) > 0.f ? 1.f / size(wave) : 0.f;
   int turn = 0;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      norm_input8<T>(v[i], a, drop, n, r,
-                     static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece, len[i]);
+      const int c = (i * kWaves + wave) * kSpan;
+      norm_input<T, kWave>(v[i], a, drop, n, r, c, lane, cols - c);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
     }
@@ -247,7 +286,8 @@ __global__ __launch_bounds__(TH) void norm_block_kernel(const NormArgs a, const 
     for (int i = 0; i < NP; ++i)
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
-        const float e = u < len[i] ? v[i][u] - part : 0.f;
+        const int c = (i * kWaves + wave) * kSpan + Span<T, kWave>::col(lane, u);
+        const float e = c < cols ? v[i][u] - part : 0.f;
         sq += e * e;
       }
     sq = wave_sum(sq);
@@ -258,27 +298,19 @@ __global__ __launch_bounds__(TH) void norm_block_kernel(const NormArgs a, const 
     __syncthreads();  // the other half of lds is free again at the next row's
     float mean = 0.f, var = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) mean += size[k] * lds[turn][k];
+    for (int k = 0; k < kWaves; ++k) mean += size(k) * lds[turn][k];
     mean *= inv;
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
       const float away = lds[turn][k] - mean;
-      var += lds[turn][kWaves + k] + size[k] * (away * away);
+      var += lds[turn][kWaves + k] + size(k) * (away * away);
     }
     const float rstd = 1.f / sqrtf(var * inv + a.eps);
-    if (threadIdx.x == 0) {
-      if (a.mean != nullptr) a.mean[r] = mean;
-      if (a.rstd != nullptr) a.rstd[r] = rstd;
-    }
+    if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
-      if (a.sum.p != nullptr)
-        store8(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v[i], len[i]);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u)
-        v[i][u] = (v[i][u] - mean) * rstd * w[i][u] + b[i][u];
-      store8(static_cast<T*>(a.out.p) + r * a.out.stride + c, v[i], len[i]);
+      const int c = (i * kWaves + wave) * kSpan;
+      norm_store<T, kWave>(v[i], a, r, c, lane, cols - c, mean, rstd, w[i], b[i]);
     }
   }
 }
@@ -323,7 +355,9 @@ static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t
   return hipGetLastError();
 }
 
-hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream) {
+hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStream_t stream) {
+  NormArgs a = args;
+  a.stream = streams(bf16, a.rows, a.cols);
   return bf16 ? launch_norm_t<uint16_t>(a, drop, stream) : launch_norm_t<float>(a, drop, stream);
 }
 
@@ -333,21 +367,40 @@ hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream
 // sum_parts_kernel adds the blocks' rows in order.
 // ---------------------------------------------------------------------------
 
-// The row's gradient from z, h = grad * weight and their means, plus what
-// reaches the sum from elsewhere; stored, dropped out for grad_x.
-template <typename T>
-__device__ __forceinline__ void store_grads8(const NormGradArgs& a, const Drop& drop, uint64_t n,
-                                             int64_t r, int64_t c, int len, float d[kLanePiece]) {
-  if (a.grad_residual.p != nullptr)
-    store8(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, len);
-  if (a.grad_x.p != nullptr) {
-    if (drop.t) drop8(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r));
-    store8(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, len);
+// What a row needs of one span, all read ahead of its sums.
+template <typename T, int G>
+struct GradSpan {
+  Span<T, G> dy, s, up;
+  __device__ __forceinline__ void load(const NormGradArgs& a, int64_t r, int64_t c, int lane,
+                                       int left) {
+    dy.load(static_cast<const T*>(a.grad.p) + r * a.grad.stride + c, lane, left);
+    s.load(static_cast<const T*>(a.s.p) + r * a.s.stride + c, lane, left);
+    if (a.grad_sum.p != nullptr)
+      up.load(static_cast<const T*>(a.grad_sum.p) + r * a.grad_sum.stride + c, lane, left);
   }
-}
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_rows8(const RowsIn& x, int64_t r, int64_t c, int len) {
-  return load_raw8(static_cast<const T*>(x.p) + r * x.stride + c, len);
+};
+
+// The row's gradient d, plus what reaches the sum from elsewhere (up); stored,
+// dropped out for grad_x.
+template <typename T, int G>
+__device__ __forceinline__ void norm_grad_store(float d[kLanePiece], const Span<T, G>& up,
+                                                const NormGradArgs& a, const Drop& drop, uint64_t n,
+                                                int64_t r, int64_t c, int lane, int left) {
+  typedef Span<T, G> S;
+  if (a.grad_sum.p != nullptr) {
+    float q[kLanePiece];
+    up.widen_to(q);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
+  }
+  if (a.grad_residual.p != nullptr)
+    S::store(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, lane, left,
+             a.stream);
+  if (a.grad_x.p != nullptr) {
+    if (drop.t)
+      S::drop(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r), lane);
+    S::store(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, lane, left, a.stream);
+  }
 }
 
 // Narrow rows, by groups of G lanes as in norm_group_kernel: a lane keeps its
@@ -356,18 +409,16 @@ template <typename T, int G, int NP>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const NormGradArgs a,
                                                                       const Drop drop,
                                                                       float* part) {
-  constexpr int kRows = kRowThreads / G;
-  __shared__ float lds[kRowWaves][G * NP * kLanePiece];
+  constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
+  __shared__ float lds[kRowWaves][NP * kSpan];
   const int lane = threadIdx.x % G, wave = threadIdx.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const float inv = 1.f / static_cast<float>(a.cols);
-  int len[NP];
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
-    len[i] = piece_len(c, a.cols);
-    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
@@ -376,13 +427,14 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
     const int64_t r = r0 + threadIdx.x / G;
     const bool mine = r < a.rows;
     const float mean = mine ? a.mean[r] : 0.f, rstd = mine ? a.rstd[r] : 0.f;
+    GradSpan<T, G> in[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) in[i].load(a, r, i * kSpan, lane, mine ? cols - i * kSpan : 0);
     float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
-      const int m = mine ? len[i] : 0;
-      widen8(dy[i], load_rows8<T>(a.grad, r, c, m));
-      widen8(z[i], load_rows8<T>(a.s, r, c, m));
+      in[i].dy.widen_to(dy[i]);
+      in[i].s.widen_to(z[i]);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
         z[i][u] = (z[i][u] - mean) * rstd;
@@ -397,17 +449,10 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
     if (!mine) continue;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * G + lane) * kLanePiece;
       float d[kLanePiece];
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
-      if (a.grad_sum.p != nullptr) {
-        float q[kLanePiece];
-        widen8(q, load_rows8<T>(a.grad_sum, r, c, len[i]));
-#pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
-      }
-      store_grads8<T>(a, drop, n, r, c, len[i], d);
+      norm_grad_store<T, G>(d, in[i].up, a, drop, n, r, i * kSpan, lane, cols - i * kSpan);
     }
   }
   if (part == nullptr) return;
@@ -422,14 +467,14 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
         float v = which ? gb[i][u] : gw[i][u];
 #pragma unroll
         for (int m = G; m < kWave; m <<= 1) v += __shfl_xor(v, m);
-        if ((threadIdx.x & (kWave - 1)) < G) lds[wave][(i * G + lane) * kLanePiece + u] = v;
+        if ((threadIdx.x & (kWave - 1)) < G) lds[wave][i * kSpan + Span<T, G>::col(lane, u)] = v;
       }
     __syncthreads();
-    for (int c = threadIdx.x; c < a.cols; c += kRowThreads) {
+    for (int c = threadIdx.x; c < cols; c += kRowThreads) {
       float v = 0.f;
 #pragma unroll
       for (int k = 0; k < kRowWaves; ++k) v += lds[k][c];
-      part[(static_cast<int64_t>(blockIdx.x) * 2 + which) * a.cols + c] = v;
+      part[(static_cast<int64_t>(blockIdx.x) * 2 + which) * cols + c] = v;
     }
   }
 }
@@ -439,30 +484,34 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
 template <typename T, int TH, int NP>
 __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs a, const Drop drop,
                                                              float* part) {
-  constexpr int kWaves = TH / kWave;
+  constexpr int kWaves = TH / kWave, kSpan = kWave * kLanePiece;
   __shared__ float lds[2][2 * kWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const float inv = 1.f / static_cast<float>(a.cols);
-  int len[NP];
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
-    len[i] = piece_len(c, a.cols);
-    load_weights8(w[i], a.weight, a.weight_bf16, c, len[i], 1.f);
+    const int c = (i * kWaves + wave) * kSpan;
+    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c, lane, cols - c, 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
   int turn = 0;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     const float mean = a.mean[r], rstd = a.rstd[r];
+    GradSpan<T, kWave> in[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (i * kWaves + wave) * kSpan;
+      in[i].load(a, r, c, lane, cols - c);
+    }
     float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
-      widen8(dy[i], load_rows8<T>(a.grad, r, c, len[i]));
-      widen8(z[i], load_rows8<T>(a.s, r, c, len[i]));
+      in[i].dy.widen_to(dy[i]);
+      in[i].s.widen_to(z[i]);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
         z[i][u] = (z[i][u] - mean) * rstd;
@@ -490,26 +539,20 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
     m2 *= inv;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
+      const int c = (i * kWaves + wave) * kSpan;
       float d[kLanePiece];
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
-      if (a.grad_sum.p != nullptr) {
-        float q[kLanePiece];
-        widen8(q, load_rows8<T>(a.grad_sum, r, c, len[i]));
-#pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
-      }
-      store_grads8<T>(a, drop, n, r, c, len[i], d);
+      norm_grad_store<T, kWave>(d, in[i].up, a, drop, n, r, c, lane, cols - c);
     }
   }
   if (part == nullptr) return;
-  float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+  float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int64_t c = static_cast<int64_t>(i * TH + threadIdx.x) * kLanePiece;
-    store8(mine + c, gw[i], len[i]);
-    store8(mine + a.cols + c, gb[i], len[i]);
+    const int c = (i * kWaves + wave) * kSpan;
+    Span<T, kWave>::store(mine + c, gw[i], lane, cols - c, false);
+    Span<T, kWave>::store(mine + cols + c, gb[i], lane, cols - c, false);
   }
 }
 
@@ -518,23 +561,27 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormGradArgs a,
                                                                      const Drop drop, float* part) {
+  constexpr int kSpan = kWave * kLanePiece;
   __shared__ float lds[2 * kRowWaves];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t begin = (threadIdx.x >> 6) * kSpan, step = kRowWaves * kSpan;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const float inv = 1.f / static_cast<float>(a.cols);
   float* pw = part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
   float* pb = pw + a.cols;
   bool first = true;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T* g = static_cast<const T*>(a.grad.p) + r * a.grad.stride;
-    const T* s = static_cast<const T*>(a.s.p) + r * a.s.stride;
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sh = 0.f, shz = 0.f;
-    for (int64_t c = threadIdx.x * kLanePiece; c < a.cols; c += kRowThreads * kLanePiece) {
-      const int len = piece_len(c, a.cols);
+    for (int64_t c = begin; c < a.cols; c += step) {
+      const int left = cols_left(c, a.cols);
+      Span<T, kWave> g, s;
       float dy[kLanePiece], z[kLanePiece], w[kLanePiece];
-      load8(dy, g + c, len);
-      load8(z, s + c, len);
-      load_weights8(w, a.weight, a.weight_bf16, c, len, 1.f);
+      g.load(static_cast<const T*>(a.grad.p) + r * a.grad.stride + c, lane, left);
+      s.load(static_cast<const T*>(a.s.p) + r * a.s.stride + c, lane, left);
+      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      g.widen_to(dy);
+      s.widen_to(z);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
         const float h = dy[u] * w[u];
@@ -544,31 +591,29 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormG
     }
     block_sum2(sh, shz, lds);
     const float m1 = sh * inv, m2 = shz * inv;
-    for (int64_t c = threadIdx.x * kLanePiece; c < a.cols; c += kRowThreads * kLanePiece) {
-      const int len = piece_len(c, a.cols);
+    for (int64_t c = begin; c < a.cols; c += step) {
+      const int left = cols_left(c, a.cols);
+      GradSpan<T, kWave> in;
       float dy[kLanePiece], z[kLanePiece], w[kLanePiece], d[kLanePiece];
-      load8(dy, g + c, len);
-      load8(z, s + c, len);
-      load_weights8(w, a.weight, a.weight_bf16, c, len, 1.f);
+      in.load(a, r, c, lane, left);
+      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      in.dy.widen_to(dy);
+      in.s.widen_to(z);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
         z[u] = (z[u] - mean) * rstd;
         d[u] = rstd * (dy[u] * w[u] - m1 - z[u] * m2);
       }
-      if (a.grad_sum.p != nullptr) {
-        float q[kLanePiece];
-        load8(q, static_cast<const T*>(a.grad_sum.p) + r * a.grad_sum.stride + c, len);
-#pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
-      }
-      store_grads8<T>(a, drop, n, r, c, len, d);
+      norm_grad_store<T, kWave>(d, in.up, a, drop, n, r, c, lane, left);
       if (part != nullptr) {
 #pragma unroll
-        for (int u = 0; u < kLanePiece; ++u)
-          if (u < len) {
-            pw[c + u] = (first ? 0.f : pw[c + u]) + dy[u] * z[u];
-            pb[c + u] = (first ? 0.f : pb[c + u]) + dy[u];
+        for (int u = 0; u < kLanePiece; ++u) {
+          const int at = Span<T, kWave>::col(lane, u);
+          if (at < left) {
+            pw[c + at] = (first ? 0.f : pw[c + at]) + dy[u] * z[u];
+            pb[c + at] = (first ? 0.f : pb[c + at]) + dy[u];
           }
+        }
       }
     }
     first = false;
@@ -659,8 +704,10 @@ static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* p
   }
 }
 
-hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, void* workspace,
+hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& drop, void* workspace,
                             hipStream_t stream) {
+  NormGradArgs a = args;
+  a.stream = streams(bf16, a.rows, a.cols);
   const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
   const int blocks = norm_grad_blocks(a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;

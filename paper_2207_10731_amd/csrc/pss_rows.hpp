@@ -43,6 +43,7 @@ struct NormArgs {
   float* mean = nullptr;
   float* rstd = nullptr;
   int64_t rows = 0, cols = 0;
+  bool stream = false;  // results are stored past the caches (set by the launcher)
 };
 
 struct NormGradArgs {
@@ -55,6 +56,7 @@ struct NormGradArgs {
   float* grad_weight = nullptr;
   float* grad_bias = nullptr;
   int64_t rows = 0, cols = 0;
+  bool stream = false;  // as in NormArgs
 };
 
 // Position buckets: `num` in all, one side's `side` borders.
@@ -74,6 +76,7 @@ struct BiasArgs {
   int64_t out_stride[3] = {0, 0, 0};
   const void* table = nullptr;
   bool table_bf16 = false;
+  bool stream = false;  // as in NormArgs
 };
 
 // Bucket of a key `rel` positions ahead of its query (rel <= 0: behind it).
@@ -124,70 +127,38 @@ __device__ __forceinline__ uint64_t drop_offset(const Drop& d) {
   return d.offset + (d.step != nullptr ? *d.step : 0u);
 }
 
-// v = D(v) for piece c8 of row r (n: drop_offset of the call).  A dropped
-// element is 0 whatever it held.
-__device__ __forceinline__ void drop8(float v[kLanePiece], const Drop& d, uint64_t n, uint32_t c8,
-                                      uint32_t r) {
-  uint32_t w[4];
-  drop_words(w, d.k0, d.k1, n, c8, r);
-#pragma unroll
-  for (int u = 0; u < kLanePiece; ++u) v[u] = drop_number(w, u) < d.t ? 0.f : v[u] * d.scale;
-}
-
-// Pieces in memory: 16-byte loads and stores at any element (the memory system
+// Vectors in memory: 16-byte loads and stores at any element (the memory system
 // takes them at any alignment of whole elements).
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t h4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint16_t h8_any __attribute__((ext_vector_type(8), aligned(2)));
 template <typename T>
-struct Raw8;
+struct Vec;  // 16 bytes of T
 template <>
-struct Raw8<float> {
-  f4_any a, b;
+struct Vec<float> {
+  typedef f4_any type;
 };
 template <>
-struct Raw8<uint16_t> {
-  h8_any a;
+struct Vec<uint16_t> {
+  typedef h8_any type;
 };
-
-// n elements from p on (8 or more: a whole piece); the others are 0.
-__device__ __forceinline__ Raw8<float> load_raw8(const float* p, int n) {
-  Raw8<float> x;
-  if (n >= kLanePiece) {
-    x.a = *reinterpret_cast<const f4_any*>(p);
-    x.b = *reinterpret_cast<const f4_any*>(p + 4);
-  } else {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      x.a[u] = u < n ? p[u] : 0.f;
-      x.b[u] = u + 4 < n ? p[u + 4] : 0.f;
-    }
-  }
-  return x;
-}
-__device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int n) {
-  Raw8<uint16_t> x;
-  if (n >= kLanePiece) {
-    x.a = *reinterpret_cast<const h8_any*>(p);
-  } else {
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) x.a[u] = u < n ? p[u] : uint16_t{0};
-  }
-  return x;
-}
-__device__ __forceinline__ void widen8(float v[kLanePiece], const Raw8<float>& x) {
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    v[u] = x.a[u];
-    v[u + 4] = x.b[u];
-  }
-}
-__device__ __forceinline__ void widen8(float v[kLanePiece], const Raw8<uint16_t>& x) {
-#pragma unroll
-  for (int u = 0; u < kLanePiece; ++u) v[u] = bf16_to_f32(x.a[u]);
-}
 template <typename T>
-__device__ __forceinline__ void load8(float v[kLanePiece], const T* p, int n) {
-  widen8(v, load_raw8(p, n));
+constexpr int kVec = 16 / static_cast<int>(sizeof(T));
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(uint16_t x) { return bf16_to_f32(x); }
+
+// Rows are read once: past the caches (their lines are not kept for others),
+// which for a large copy of float32 is 6.2 against 5.8 TB/s.  n elements from p
+// on (kVec or more: all); the others are 0.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::type load_vec(const T* p, int n) {
+  typedef typename Vec<T>::type V;
+  if (n >= kVec<T>) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  V x;
+#pragma unroll
+  for (int u = 0; u < kVec<T>; ++u) x[u] = u < n ? p[u] : T{0};
+  return x;
 }
 
 // Two floats as bfloat16 bits, to nearest even (one instruction).
@@ -199,52 +170,133 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   __builtin_memcpy(&u, &b, 4);
   return u;
 }
-
-__device__ __forceinline__ void store8(float* p, const float v[kLanePiece], int n) {
-  if (n >= kLanePiece) {
-    f4_any a, b;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      a[u] = v[u];
-      b[u] = v[u + 4];
-    }
-    *reinterpret_cast<f4_any*>(p) = a;
-    *reinterpret_cast<f4_any*>(p + 4) = b;
-  } else {
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u)
-      if (u < n) p[u] = v[u];
-  }
+__device__ __forceinline__ f4_any narrow(const float* v, float) {
+  return f4_any{v[0], v[1], v[2], v[3]};
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float v[kLanePiece], int n) {
+__device__ __forceinline__ h8_any narrow(const float* v, uint16_t) {
   h8_any a;
 #pragma unroll
-  for (int u = 0; u < kLanePiece; u += 2) {
+  for (int u = 0; u < 8; u += 2) {
     const uint32_t w = bf16_pair(v[u], v[u + 1]);
     a[u] = static_cast<uint16_t>(w);
     a[u + 1] = static_cast<uint16_t>(w >> 16);
   }
-  if (n >= kLanePiece) {
-    *reinterpret_cast<h8_any*>(p) = a;
+  return a;
+}
+// stream: past the caches (results too large for them).
+template <typename T>
+__device__ __forceinline__ void store_vec(T* p, const float* v, int n, bool stream) {
+  typedef typename Vec<T>::type V;
+  const V a = narrow(v, T{});
+  if (n >= kVec<T>) {
+    if (stream)
+      __builtin_nontemporal_store(a, reinterpret_cast<V*>(p));
+    else
+      *reinterpret_cast<V*>(p) = a;
   } else {
 #pragma unroll
-    for (int u = 0; u < kLanePiece; ++u)
+    for (int u = 0; u < kVec<T>; ++u)
       if (u < n) p[u] = a[u];
   }
 }
 
-// Weights (bf16: their storage) of a piece; null: `fill`.
-__device__ __forceinline__ void load_weights8(float v[kLanePiece], const void* w, bool bf16,
-                                              int64_t c, int n, float fill) {
-  if (w == nullptr) {
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] = fill;
-  } else if (bf16) {
-    load8(v, static_cast<const uint16_t*>(w) + c, n);
-  } else {
-    load8(v, static_cast<const float*>(w) + c, n);
+// A span: G * 8 consecutive columns of a row, 8 of them to each of G
+// neighbouring lanes, laid out so that the lanes of one load or store are
+// 16 bytes apart: a bfloat16 lane has columns 8 lane .. 8 lane + 7, a float32 lane
+// 4 lane .. 4 lane + 3 and the same of the span's second half (32 bytes apart a
+// large float32 copy runs at 5.2 to 5.9 TB/s, 16 apart at 5.8 to 6.2).
+template <typename T, int G>
+struct Span {
+  static constexpr int kParts = kLanePiece / kVec<T>;
+  typename Vec<T>::type q[kParts];
+
+  static __device__ __forceinline__ int col(int lane, int u) {
+    return u / kVec<T> * (G * kVec<T>) + lane * kVec<T> + u % kVec<T>;
   }
-}
+  // p: the span's first column; left: columns from there to the row's end.
+  __device__ __forceinline__ void load(const T* p, int lane, int left) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int c = col(lane, i * kVec<T>);
+      q[i] = load_vec(p + c, left - c);
+    }
+  }
+  __device__ __forceinline__ void widen_to(float v[kLanePiece]) const {
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) v[u] = widen(q[u / kVec<T>][u % kVec<T>]);
+  }
+  template <typename O>
+  static __device__ __forceinline__ void store(O* p, const float v[kLanePiece], int lane, int left,
+                                               bool stream) {
+    constexpr int V = kVec<O> < kVec<T> ? kVec<O> : kVec<T>;  // consecutive columns
+#pragma unroll
+    for (int u = 0; u < kLanePiece; u += V)
+      store_vec(p + col(lane, u), v + u, left - col(lane, u), stream);
+  }
+  // Weights (bf16: their storage) from column c0 on in the span's layout; null:
+  // `fill`.  Other blocks read them too: through the caches, in fours.
+  static __device__ __forceinline__ void weights(float v[kLanePiece], const void* w, bool bf16,
+                                                 int64_t c0, int lane, int left, float fill) {
+#pragma unroll
+    for (int u = 0; u < kLanePiece; u += 4) {
+      const int c = col(lane, u);
+      const bool whole = c + 4 <= left;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u + k] = fill;
+      if (w == nullptr) continue;
+      if (bf16) {
+        const uint16_t* p = static_cast<const uint16_t*>(w) + c0 + c;
+        if (whole) {
+          const h4_any x = *reinterpret_cast<const h4_any*>(p);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u + k] = bf16_to_f32(x[k]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k < left) v[u + k] = bf16_to_f32(p[k]);
+        }
+      } else {
+        const float* p = static_cast<const float*>(w) + c0 + c;
+        if (whole) {
+          const f4_any x = *reinterpret_cast<const f4_any*>(p);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u + k] = x[k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k < left) v[u + k] = p[k];
+        }
+      }
+    }
+  }
+  // v = D(v) in row r of the span at piece c8 (n: drop_offset of the call).  A
+  // dropped element is 0 whatever it held.  A float32 lane has halves of two
+  // pieces, which a pair of lanes shares: the even lane makes the numbers of the
+  // first, the odd one those of the second, and they exchange halves.  The
+  // lanes of a group take part together.
+  static __device__ __forceinline__ void drop(float v[kLanePiece], const Drop& d, uint64_t n,
+                                              uint32_t c8, uint32_t r, int lane) {
+    uint32_t w[4];
+    if constexpr (kParts == 1 || G == 1) {
+      drop_words(w, d.k0, d.k1, n, c8 + lane, r);
+    } else {
+      const bool odd = lane & 1;
+      drop_words(w, d.k0, d.k1, n, c8 + (odd ? G / 2 : 0) + lane / 2, r);
+      const uint32_t give0 = odd ? w[0] : w[2], give1 = odd ? w[1] : w[3];
+      const uint32_t got0 = __builtin_amdgcn_update_dpp(0, give0, 0xb1, 0xf, 0xf, true);
+      const uint32_t got1 = __builtin_amdgcn_update_dpp(0, give1, 0xb1, 0xf, 0xf, true);
+      if (odd) {
+        w[0] = got0;
+        w[1] = got1;
+      } else {
+        w[2] = got0;
+        w[3] = got1;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) v[u] = drop_number(w, u) < d.t ? 0.f : v[u] * d.scale;
+  }
+};
 
 // Sum over groups of G neighbouring lanes (a power of two), the same bits in
 // every lane of a group; every lane of the wavefront takes part.  Within 16
@@ -282,8 +334,8 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, 
 // Relative position bias (pss_bias.hip); every size > 0.
 hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipStream_t stream);
 // bias_grad_fits: as many blocks as a grid can have.
-bool bias_grad_fits(const BiasArgs& a, const BucketMap& map);
-size_t bias_grad_workspace_bytes(const BiasArgs& a, const BucketMap& map);
+bool bias_grad_fits(bool bf16, const BiasArgs& a, const BucketMap& map);
+size_t bias_grad_workspace_bytes(bool bf16, const BiasArgs& a, const BucketMap& map);
 hipError_t launch_bias_grad(bool bf16, const BiasArgs& a, const BucketMap& map, void* workspace,
                             float* grad_table, hipStream_t stream);
 

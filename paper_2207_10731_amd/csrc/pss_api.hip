@@ -1112,8 +1112,10 @@ int pss_layer_norm_backward(const pss_rows_params* params, const pss_dropout_par
   a.rows = params->rows;
   a.cols = params->cols;
   CallScratch scratch;
-  if (grad_weight != nullptr || grad_bias != nullptr) {
-    st = scratch.take(pss::norm_grad_workspace_bytes(a.rows, a.cols), stream);
+  const size_t need = pss::norm_grad_workspace_bytes(
+      a.rows, a.cols, grad_weight != nullptr || grad_bias != nullptr);
+  if (need > 0) {
+    st = scratch.take(need, stream);
     if (st != PSS_OK) return st;
   }
   const hipError_t e =

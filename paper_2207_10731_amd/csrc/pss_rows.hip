@@ -6,26 +6,8 @@ namespace pss {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / kWave;
-constexpr int kNormBlocks = 256 * 8;  // blocks that walk rows: 8 to a CU
-
-// Sums of two values over the block, in every thread, in a fixed order.
-__device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
-  a = wave_sum(a);
-  b = wave_sum(b);
-  const int w = threadIdx.x >> 6;
-  __syncthreads();  // the last values are read
-  if ((threadIdx.x & (kWave - 1)) == 0) {
-    lds[w] = a;
-    lds[kRowWaves + w] = b;
-  }
-  __syncthreads();
-  a = b = 0.f;
-#pragma unroll
-  for (int i = 0; i < kRowWaves; ++i) {
-    a += lds[i];
-    b += lds[kRowWaves + i];
-  }
-}
+constexpr int kMaxWaves = 16;  // of a block that takes a row together
+constexpr int kSpanCols = kWave * kLanePiece;  // columns of a wavefront's span
 
 // Columns from c on, as an int (a span has at most 512).
 __device__ __forceinline__ int cols_left(int64_t c, int64_t cols) {
@@ -111,28 +93,37 @@ hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, co
 }
 
 // ---------------------------------------------------------------------------
-// Layer norm.
+// Layer norm.  Rows of up to 16384 columns are read once and stay in
+// registers: up to 1024 columns a group of lanes takes a row, beyond that a block
+// of as many wavefronts as the row fills.  Groups and blocks walk over rows, with
+// the row after the present one already requested and the weights in
+// registers.  Bound by memory: 2 to 4 row arrays read or written.
 // ---------------------------------------------------------------------------
 
-// s of one span: residual + D(x).
+// What a row needs of one span.
 template <typename T, int G>
-__device__ __forceinline__ void norm_input(float v[kLanePiece], const NormArgs& a, const Drop& drop,
-                                           uint64_t n, int64_t r, int64_t c, int lane, int left) {
+struct NormSpan {
   Span<T, G> x, q;
-  x.load(static_cast<const T*>(a.x.p) + r * a.x.stride + c, lane, left);
-  if (a.residual.p != nullptr)
-    q.load(static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, lane, left);
-  x.widen_to(v);
-  if (drop.t)
-    Span<T, G>::drop(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r),
-                     lane);
-  if (a.residual.p != nullptr) {
-    float w[kLanePiece];
-    q.widen_to(w);
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) v[u] += w[u];
+  __device__ __forceinline__ void load(const NormArgs& a, int64_t r, int64_t c, int lane, int left) {
+    x.load(static_cast<const T*>(a.x.p) + r * a.x.stride + c, lane, left);
+    if (a.residual.p != nullptr)
+      q.load(static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, lane, left);
   }
-}
+  // s = residual + D(x)
+  __device__ __forceinline__ void sum_to(float v[kLanePiece], const NormArgs& a, const Drop& drop,
+                                         uint64_t n, int64_t r, int64_t c, int lane) const {
+    x.widen_to(v);
+    if (drop.t)
+      Span<T, G>::drop(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r),
+                       lane);
+    if (a.residual.p != nullptr) {
+      float w[kLanePiece];
+      q.widen_to(w);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) v[u] += w[u];
+    }
+  }
+};
 
 template <typename T, int G>
 __device__ __forceinline__ void norm_store(float v[kLanePiece], const NormArgs& a, int64_t r,
@@ -146,50 +137,218 @@ __device__ __forceinline__ void norm_store(float v[kLanePiece], const NormArgs& 
   S::store(static_cast<T*>(a.out.p) + r * a.out.stride + c, v, lane, left, a.stream);
 }
 
-__device__ __forceinline__ void norm_store_stats(const NormArgs& a, int64_t r, float mean, float rstd) {
+__device__ __forceinline__ void norm_store_stats(const NormArgs& a, int64_t r, float mean,
+                                                 float rstd) {
   if (a.mean != nullptr) a.mean[r] = mean;
   if (a.rstd != nullptr) a.rstd[r] = rstd;
 }
 
-// Rows of any width: a block a row, which it reads three times (sum, squares
-// about the mean, result).  Nothing is stored before the last pass, where
-// every element is read by the lane that then stores its results.
+// Squares of a span's elements about `mean`.
+template <typename T, int G>
+__device__ __forceinline__ float squares(const float v[kLanePiece], int lane, int left, float mean) {
+  float sq = 0.f;
+#pragma unroll
+  for (int u = 0; u < kLanePiece; ++u) {
+    const float e = Span<T, G>::col(lane, u) < left ? v[u] - mean : 0.f;
+    sq += e * e;
+  }
+  return sq;
+}
+
+// A group of G lanes a row, NP spans.  AHEAD: the next row is requested before the
+// present one's sums.  (4 wavefronts to a SIMD: at most 128 registers.)
+template <typename T, int G, int NP, bool AHEAD>
+__global__ __launch_bounds__(kRowThreads, 4) void norm_group_kernel(const NormArgs a, const Drop drop) {
+  constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
+  const int lane = threadIdx.x % G;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / G;
+  NormSpan<T, G> in[NP], next[NP];
+  float w[NP][kLanePiece], b[NP][kLanePiece];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    in[i].load(a, r, i * kSpan, lane, r < a.rows ? cols - i * kSpan : 0);
+    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
+    Span<T, G>::weights(b[i], a.bias, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 0.f);
+  }
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows; r0 += step, r += step) {
+    if (AHEAD && r0 + step < a.rows) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        next[i].load(a, r + step, i * kSpan, lane, r + step < a.rows ? cols - i * kSpan : 0);
+    }
+    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      in[i].sum_to(v[i], a, drop, n, r, i * kSpan, lane);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
+    }
+    const float mean = group_sum<G>(sum) * inv;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) sq += squares<T, G>(v[i], lane, cols - i * kSpan, mean);
+    const float rstd = 1.f / sqrtf(group_sum<G>(sq) * inv + a.eps);
+    if (r < a.rows) {
+      if (lane == 0) norm_store_stats(a, r, mean, rstd);
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        norm_store<T, G>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      if (AHEAD)
+        in[i] = next[i];
+      else
+        in[i].load(a, r + step, i * kSpan, lane, r + step < a.rows ? cols - i * kSpan : 0);
+    }
+  }
+}
+
+// Wavefront k of n has the spans at columns (i n + k) * kSpanCols, i < NP: how many
+// elements of a row of `cols`.
+template <int NP>
+__device__ __forceinline__ float part_size(int k, int n, int cols) {
+  int e = 0;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int left = cols - (i * n + k) * kSpanCols;
+    e += left < 0 ? 0 : (left > kSpanCols ? kSpanCols : left);
+  }
+  return static_cast<float>(e);
+}
+
+// A block a row.  Every wavefront takes mean and squares of its own part; the
+// parts are joined through LDS with one barrier a row (the squares about the
+// common mean are those about each part's plus the part's size times the square
+// of its mean's distance).
+template <typename T, int TH, int NP, bool AHEAD>
+__global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, const Drop drop) {
+  __shared__ float lds[2][2][kMaxWaves];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const int cols = static_cast<int>(a.cols);
+  const float inv = 1.f / static_cast<float>(cols);
+  int64_t r = blockIdx.x;
+  NormSpan<T, kWave> in[NP], next[NP];
+  float w[NP][kLanePiece], b[NP][kLanePiece];
+  int c[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    c[i] = (i * waves + wave) * kSpanCols;
+    in[i].load(a, r, c[i], lane, cols - c[i]);
+    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
+    Span<T, kWave>::weights(b[i], a.bias, a.weight_bf16, c[i], lane, cols - c[i], 0.f);
+  }
+  const float my_size = part_size<NP>(wave, waves, cols);
+  const float inv_part = my_size > 0.f ? 1.f / my_size : 0.f;
+  const int other = lane % kMaxWaves;  // the part this lane joins
+  const float size = other < waves ? part_size<NP>(other, waves, cols) : 0.f;
+  int turn = 0;
+  for (; r < a.rows; r += gridDim.x, turn ^= 1) {
+    const int64_t after = r + gridDim.x;
+    if (AHEAD && after < a.rows) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) next[i].load(a, after, c[i], lane, cols - c[i]);
+    }
+    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      in[i].sum_to(v[i], a, drop, n, r, c[i], lane);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
+    }
+    const float part = wave_sum(sum) * inv_part;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) sq += squares<T, kWave>(v[i], lane, cols - c[i], part);
+    sq = wave_sum(sq);
+    if (lane == 0) {
+      lds[turn][0][wave] = part;
+      lds[turn][1][wave] = sq;
+    }
+    __syncthreads();  // the other half of lds is free again at the next row's
+    const float their_mean = other < waves ? lds[turn][0][other] : 0.f;
+    const float their_sq = other < waves ? lds[turn][1][other] : 0.f;
+    const float mean = group_sum<kMaxWaves>(size * their_mean) * inv;
+    const float away = their_mean - mean;
+    const float var = group_sum<kMaxWaves>(their_sq + size * (away * away)) * inv;
+    const float rstd = 1.f / sqrtf(var + a.eps);
+    if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      norm_store<T, kWave>(v[i], a, r, c[i], lane, cols - c[i], mean, rstd, w[i], b[i]);
+      if (AHEAD)
+        in[i] = next[i];
+      else if (after < a.rows)
+        in[i].load(a, after, c[i], lane, cols - c[i]);
+    }
+  }
+}
+
+// Sums of two values over the block, in every thread, in a fixed order.
+__device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  const int w = threadIdx.x >> 6;
+  __syncthreads();  // the last values are read
+  if ((threadIdx.x & (kWave - 1)) == 0) {
+    lds[w] = a;
+    lds[kRowWaves + w] = b;
+  }
+  __syncthreads();
+  a = b = 0.f;
+#pragma unroll
+  for (int i = 0; i < kRowWaves; ++i) {
+    a += lds[i];
+    b += lds[kRowWaves + i];
+  }
+}
+
+// Wider rows: a block a row, which it reads three times (sum, squares about the
+// mean, result), the last two from L2.  Nothing is stored before the last pass,
+// where every element is read by the lane that then stores its results.
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void norm_wide_kernel(const NormArgs a, const Drop drop) {
-  constexpr int kSpan = kWave * kLanePiece;
+__global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2 * kRowWaves];
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t first = (threadIdx.x >> 6) * kSpan, step = kRowWaves * kSpan;
+  const int64_t first = (threadIdx.x >> 6) * kSpanCols, step = kRowWaves * kSpanCols;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const float inv = 1.f / static_cast<float>(a.cols);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     float sum = 0.f, zero = 0.f;
+#pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
+      NormSpan<T, kWave> in;
       float v[kLanePiece];
-      norm_input<T, kWave>(v, a, drop, n, r, c, lane, cols_left(c, a.cols));
+      in.load(a, r, c, lane, cols_left(c, a.cols));
+      in.sum_to(v, a, drop, n, r, c, lane);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[u];
     }
     block_sum2(sum, zero, lds);
     const float mean = sum * inv;
     float sq = 0.f;
+#pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
+      NormSpan<T, kWave> in;
       float v[kLanePiece];
-      const int left = cols_left(c, a.cols);
-      norm_input<T, kWave>(v, a, drop, n, r, c, lane, left);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        const float e = Span<T, kWave>::col(lane, u) < left ? v[u] - mean : 0.f;
-        sq += e * e;
-      }
+      in.load(a, r, c, lane, cols_left(c, a.cols));
+      in.sum_to(v, a, drop, n, r, c, lane);
+      sq += squares<T, kWave>(v, lane, cols_left(c, a.cols), mean);
     }
     block_sum2(sq, zero, lds);
     const float rstd = 1.f / sqrtf(sq * inv + a.eps);
     if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
+#pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
+      NormSpan<T, kWave> in;
       float v[kLanePiece], w[kLanePiece], b[kLanePiece];
       const int left = cols_left(c, a.cols);
-      norm_input<T, kWave>(v, a, drop, n, r, c, lane, left);
+      in.load(a, r, c, lane, left);
+      in.sum_to(v, a, drop, n, r, c, lane);
       Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
       Span<T, kWave>::weights(b, a.bias, a.weight_bf16, c, lane, left, 0.f);
       norm_store<T, kWave>(v, a, r, c, lane, left, mean, rstd, w, b);
@@ -197,162 +356,66 @@ __global__ __launch_bounds__(kRowThreads) void norm_wide_kernel(const NormArgs a
   }
 }
 
-// Rows whose elements stay in registers, by groups of G lanes of a wavefront
-// (G * NP pieces cover a row): read once, mean and squares about it from the
-// registers.  A group walks its rows with its weights in registers.
-template <typename T, int G, int NP>
-__global__ __launch_bounds__(kRowThreads) void norm_group_kernel(const NormArgs a, const Drop drop) {
-  constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
-  const int lane = threadIdx.x % G;
-  const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const int cols = static_cast<int>(a.cols);
-  const float inv = 1.f / static_cast<float>(cols);
-  float w[NP][kLanePiece], b[NP][kLanePiece];
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
-    Span<T, G>::weights(b[i], a.bias, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 0.f);
-  }
-  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
-       r0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int64_t r = r0 + threadIdx.x / G;
-    const bool mine = r < a.rows;
-    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      norm_input<T, G>(v[i], a, drop, n, r, i * kSpan, lane, mine ? cols - i * kSpan : 0);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
-    }
-    const float mean = group_sum<G>(sum) * inv;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        const float e = i * kSpan + Span<T, G>::col(lane, u) < cols ? v[i][u] - mean : 0.f;
-        sq += e * e;
-      }
-    const float rstd = 1.f / sqrtf(group_sum<G>(sq) * inv + a.eps);
-    if (!mine) continue;
-    if (lane == 0) norm_store_stats(a, r, mean, rstd);
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-      norm_store<T, G>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
-  }
+// Which kernel takes rows of `cols` columns, and how many of its wavefronts a
+// CU holds (by their registers).
+struct RowForm {
+  int lanes;  // of a row: a group (<= 64), else a block of that many threads
+  int spans;  // of a lane; 0: the wide kernel
+  int waves;  // of a CU
+};
+// waves1, waves2: those of the kernels with one and two spans a lane; most:
+// wavefronts of a block.
+static RowForm row_form(int64_t cols, int waves1, int waves2, int most) {
+  const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
+  if (n <= kWave) return {row_lanes(cols), 1, waves1};
+  if (n <= 2 * kWave) return {kWave, 2, waves2};
+  // a block of whole wavefronts, one or two spans a lane: what keeps more
+  // spans on a CU
+  const int64_t w1 = (n + kWave - 1) / kWave, w2 = (n + 2 * kWave - 1) / (2 * kWave);
+  const int64_t held1 = w1 <= most ? waves1 / w1 * w1 : 0;
+  const int64_t held2 = w2 <= most ? 2 * (waves2 / w2 * w2) : 0;
+  if (held1 == 0 && held2 == 0) return {kRowThreads, 0, kRowWaves};
+  if (held1 >= held2) return {static_cast<int>(w1) * kWave, 1, waves1};
+  return {static_cast<int>(w2) * kWave, 2, waves2};
 }
-
-// The same by a whole block a row.  Every wavefront takes mean and squares of
-// its own part; the parts are joined through LDS with one barrier a row (the
-// squares about the common mean are those about each part's plus the part's
-// size times the square of its mean's distance).
-template <typename T, int TH, int NP>
-__global__ __launch_bounds__(TH) void norm_block_kernel(const NormArgs a, const Drop drop) {
-  constexpr int kWaves = TH / kWave, kSpan = kWave * kLanePiece;
-  __shared__ float lds[2][2 * kWaves];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-  const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const int cols = static_cast<int>(a.cols);
-  const float inv = 1.f / static_cast<float>(cols);
-  float w[NP][kLanePiece], b[NP][kLanePiece];
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int c = (i * kWaves + wave) * kSpan;
-    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c, lane, cols - c, 1.f);
-    Span<T, kWave>::weights(b[i], a.bias, a.weight_bf16, c, lane, cols - c, 0.f);
-  }
-  // elements of wavefront k's part
-  const auto size = [&](int k) {
-    int e = 0;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int left = cols - (i * kWaves + k) * kSpan;
-      e += left < 0 ? 0 : (left > kSpan ? kSpan : left);
-    }
-    return static_cast<float>(e);
-  };
-  const float inv_part = size(wave) > 0.f ? 1.f / size(wave) : 0.f;
-  int turn = 0;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
-    float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (i * kWaves + wave) * kSpan;
-      norm_input<T, kWave>(v[i], a, drop, n, r, c, lane, cols - c);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
-    }
-    const float part = wave_sum(sum) * inv_part;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        const int c = (i * kWaves + wave) * kSpan + Span<T, kWave>::col(lane, u);
-        const float e = c < cols ? v[i][u] - part : 0.f;
-        sq += e * e;
-      }
-    sq = wave_sum(sq);
-    if (lane == 0) {
-      lds[turn][wave] = part;
-      lds[turn][kWaves + wave] = sq;
-    }
-    __syncthreads();  // the other half of lds is free again at the next row's
-    float mean = 0.f, var = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) mean += size(k) * lds[turn][k];
-    mean *= inv;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      const float away = lds[turn][k] - mean;
-      var += lds[turn][kWaves + k] + size(k) * (away * away);
-    }
-    const float rstd = 1.f / sqrtf(var * inv + a.eps);
-    if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (i * kWaves + wave) * kSpan;
-      norm_store<T, kWave>(v[i], a, r, c, lane, cols - c, mean, rstd, w[i], b[i]);
-    }
-  }
-}
-
-static uint32_t row_grid(int64_t rows, int per_block, int most) {
+// Blocks that walk rows: what the CUs hold, with as many rows to each (a second
+// round of blocks would take as long as the first).
+static uint32_t row_blocks(const RowForm& f, int64_t rows) {
+  const bool group = f.lanes <= kWave;
+  const int64_t per_block = group ? kRowThreads / f.lanes : 1;
   const int64_t want = (rows + per_block - 1) / per_block;
-  return static_cast<uint32_t>(want < most ? want : most);
-}
-
-template <typename T, int G, int NP>
-static hipError_t launch_norm_group(const NormArgs& a, const Drop& drop, hipStream_t stream) {
-  hipLaunchKernelGGL((norm_group_kernel<T, G, NP>),
-                     dim3(row_grid(a.rows, kRowThreads / G, kNormBlocks)), dim3(kRowThreads), 0,
-                     stream, a, drop);
-  return hipGetLastError();
-}
-template <typename T, int TH, int NP>
-static hipError_t launch_norm_block(const NormArgs& a, const Drop& drop, hipStream_t stream) {
-  hipLaunchKernelGGL((norm_block_kernel<T, TH, NP>),
-                     dim3(row_grid(a.rows, 1, kNormBlocks * kRowThreads / TH)), dim3(TH), 0, stream,
-                     a, drop);
-  return hipGetLastError();
+  const int64_t held = int64_t{256} * (f.waves * kWave / (group ? kRowThreads : f.lanes));
+  const int64_t rounds = (want + held - 1) / held;
+  return static_cast<uint32_t>((want + rounds - 1) / rounds);
 }
 
 template <typename T>
 static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t stream) {
-  const int64_t pieces = (a.cols + kLanePiece - 1) / kLanePiece;
-  if (pieces <= 1) return launch_norm_group<T, 1, 1>(a, drop, stream);
-  if (pieces <= 2) return launch_norm_group<T, 2, 1>(a, drop, stream);
-  if (pieces <= 4) return launch_norm_group<T, 4, 1>(a, drop, stream);
-  if (pieces <= 8) return launch_norm_group<T, 8, 1>(a, drop, stream);
-  if (pieces <= 16) return launch_norm_group<T, 16, 1>(a, drop, stream);
-  if (pieces <= 32) return launch_norm_group<T, 32, 1>(a, drop, stream);
-  if (pieces <= 64) return launch_norm_group<T, 64, 1>(a, drop, stream);
-  if (pieces <= 128) return launch_norm_group<T, 64, 2>(a, drop, stream);
-  if (pieces <= 256) return launch_norm_block<T, 256, 1>(a, drop, stream);
-  if (pieces <= 512) return launch_norm_block<T, 256, 2>(a, drop, stream);
-  if (pieces <= 1024) return launch_norm_block<T, 512, 2>(a, drop, stream);
-  if (pieces <= 2048) return launch_norm_block<T, 1024, 2>(a, drop, stream);
-  hipLaunchKernelGGL(norm_wide_kernel<T>, dim3(row_grid(a.rows, 1, kNormBlocks)), dim3(kRowThreads), 0,
-                     stream, a, drop);
-  return hipGetLastError();
+  // 128 registers a lane at most: 16 wavefronts to a CU
+  const RowForm f = row_form(a.cols, 16, 16, kMaxWaves);
+  const dim3 grid(f.spans ? row_blocks(f, a.rows) : static_cast<uint32_t>(a.rows < 2048 ? a.rows : 2048));
+  const dim3 block(f.lanes <= kWave ? kRowThreads : f.lanes);
+  constexpr bool kAhead2 = sizeof(T) == 2;  // two float32 spans ahead: too many registers
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop);
+    return hipGetLastError();
+  };
+  if (f.spans == 0) return launch(norm_wide_kernel<T>);
+  if (f.lanes > kWave) {
+    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, 1, true>);
+    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, 2, kAhead2>)
+                          : launch(norm_block_kernel<T, 1024, 2, false>);
+  }
+  switch (f.lanes * f.spans) {
+    case 1: return launch(norm_group_kernel<T, 1, 1, true>);
+    case 2: return launch(norm_group_kernel<T, 2, 1, true>);
+    case 4: return launch(norm_group_kernel<T, 4, 1, true>);
+    case 8: return launch(norm_group_kernel<T, 8, 1, true>);
+    case 16: return launch(norm_group_kernel<T, 16, 1, true>);
+    case 32: return launch(norm_group_kernel<T, 32, 1, true>);
+    case 64: return launch(norm_group_kernel<T, 64, 1, true>);
+    default: return launch(norm_group_kernel<T, 64, 2, kAhead2>);
+  }
 }
 
 hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStream_t stream) {
@@ -363,11 +426,12 @@ hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStr
 
 // ---------------------------------------------------------------------------
 // Backward.  Each block adds what its rows give to the weight's and bias's
-// gradients to its own row of `part` ([blocks][2][cols]), and
-// sum_parts_kernel adds the blocks' rows in order.
+// gradients in registers and writes them to its own row of `part`
+// ([blocks][2][cols]); sum_parts_kernel adds the blocks' rows in order.
+// Bound by memory: 3 to 5 row arrays.
 // ---------------------------------------------------------------------------
 
-// What a row needs of one span, all read ahead of its sums.
+// What a row needs of one span.
 template <typename T, int G>
 struct GradSpan {
   Span<T, G> dy, s, up;
@@ -378,33 +442,58 @@ struct GradSpan {
     if (a.grad_sum.p != nullptr)
       up.load(static_cast<const T*>(a.grad_sum.p) + r * a.grad_sum.stride + c, lane, left);
   }
+  // The row's two sums, and this span's part of the gradients over rows.
+  __device__ __forceinline__ void sums(const float w[kLanePiece], float mean, float rstd, float& sh,
+                                       float& shz, float gw[kLanePiece],
+                                       float gb[kLanePiece]) const {
+    float d[kLanePiece], z[kLanePiece];
+    dy.widen_to(d);
+    s.widen_to(z);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) {
+      z[u] = (z[u] - mean) * rstd;
+      const float h = d[u] * w[u];
+      sh += h;
+      shz += h * z[u];
+      gw[u] += d[u] * z[u];
+      gb[u] += d[u];
+    }
+  }
+  // The row's gradient from the means m1 of h and m2 of h * z, plus what
+  // reaches the sum from elsewhere; stored, dropped out for grad_x.  (h and z
+  // are made again: registers for them cost more than the arithmetic.)
+  __device__ __forceinline__ void finish(const float w[kLanePiece], float mean, float rstd, float m1,
+                                         float m2, const NormGradArgs& a, const Drop& drop,
+                                         uint64_t n, int64_t r, int64_t c, int lane, int left) {
+    typedef Span<T, G> S;
+    float d[kLanePiece], z[kLanePiece];
+    dy.renew();
+    s.renew();
+    dy.widen_to(d);
+    s.widen_to(z);
+#pragma unroll
+    for (int u = 0; u < kLanePiece; ++u) {
+      z[u] = (z[u] - mean) * rstd;
+      d[u] = rstd * (d[u] * w[u] - m1 - z[u] * m2);
+    }
+    if (a.grad_sum.p != nullptr) {
+      up.widen_to(z);
+#pragma unroll
+      for (int u = 0; u < kLanePiece; ++u) d[u] += z[u];
+    }
+    if (a.grad_residual.p != nullptr)
+      S::store(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, lane, left,
+               a.stream);
+    if (a.grad_x.p != nullptr) {
+      if (drop.t)
+        S::drop(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r), lane);
+      S::store(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, lane, left, a.stream);
+    }
+  }
 };
 
-// The row's gradient d, plus what reaches the sum from elsewhere (up); stored,
-// dropped out for grad_x.
-template <typename T, int G>
-__device__ __forceinline__ void norm_grad_store(float d[kLanePiece], const Span<T, G>& up,
-                                                const NormGradArgs& a, const Drop& drop, uint64_t n,
-                                                int64_t r, int64_t c, int lane, int left) {
-  typedef Span<T, G> S;
-  if (a.grad_sum.p != nullptr) {
-    float q[kLanePiece];
-    up.widen_to(q);
-#pragma unroll
-    for (int u = 0; u < kLanePiece; ++u) d[u] += q[u];
-  }
-  if (a.grad_residual.p != nullptr)
-    S::store(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, lane, left,
-             a.stream);
-  if (a.grad_x.p != nullptr) {
-    if (drop.t)
-      S::drop(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r), lane);
-    S::store(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, lane, left, a.stream);
-  }
-}
-
-// Narrow rows, by groups of G lanes as in norm_group_kernel: a lane keeps its
-// columns' weights and gradient sums in registers for all of its rows.
+// A group of G lanes a row, as in norm_group_kernel; a lane keeps its columns'
+// weights and gradient sums for all of its rows.
 template <typename T, int G, int NP>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const NormGradArgs a,
                                                                       const Drop drop,
@@ -415,45 +504,43 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / G;
+  GradSpan<T, G> in[NP], next[NP];
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
+    in[i].load(a, r, i * kSpan, lane, r < a.rows ? cols - i * kSpan : 0);
     Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
-  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
-       r0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int64_t r = r0 + threadIdx.x / G;
-    const bool mine = r < a.rows;
-    const float mean = mine ? a.mean[r] : 0.f, rstd = mine ? a.rstd[r] : 0.f;
-    GradSpan<T, G> in[NP];
+  float mean = r < a.rows ? a.mean[r] : 0.f, rstd = r < a.rows ? a.rstd[r] : 0.f;
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows; r0 += step, r += step) {
+    float next_mean = 0.f, next_rstd = 0.f;
+    if (r0 + step < a.rows) {
+      const bool more = r + step < a.rows;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) in[i].load(a, r, i * kSpan, lane, mine ? cols - i * kSpan : 0);
-    float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      in[i].dy.widen_to(dy[i]);
-      in[i].s.widen_to(z[i]);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        z[i][u] = (z[i][u] - mean) * rstd;
-        const float h = dy[i][u] * w[i][u];
-        sh += h;
-        shz += h * z[i][u];
-        gw[i][u] += dy[i][u] * z[i][u];
-        gb[i][u] += dy[i][u];
+      for (int i = 0; i < NP; ++i)
+        next[i].load(a, r + step, i * kSpan, lane, more ? cols - i * kSpan : 0);
+      if (more) {
+        next_mean = a.mean[r + step];
+        next_rstd = a.rstd[r + step];
       }
     }
+    float sh = 0.f, shz = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i]);
     const float m1 = group_sum<G>(sh) * inv, m2 = group_sum<G>(shz) * inv;
-    if (!mine) continue;
+    if (r < a.rows) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      float d[kLanePiece];
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
-      norm_grad_store<T, G>(d, in[i].up, a, drop, n, r, i * kSpan, lane, cols - i * kSpan);
+      for (int i = 0; i < NP; ++i)
+        in[i].finish(w[i], mean, rstd, m1, m2, a, drop, n, r, i * kSpan, lane, cols - i * kSpan);
     }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) in[i] = next[i];
+    mean = next_mean;
+    rstd = next_rstd;
   }
   if (part == nullptr) return;
   // the groups of a wavefront, then the wavefronts
@@ -484,92 +571,72 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
 template <typename T, int TH, int NP>
 __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs a, const Drop drop,
                                                              float* part) {
-  constexpr int kWaves = TH / kWave, kSpan = kWave * kLanePiece;
-  __shared__ float lds[2][2 * kWaves];
+  __shared__ float lds[2][2][kMaxWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
+  int64_t r = blockIdx.x;
+  GradSpan<T, kWave> in[NP], next[NP];
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
+  int c[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int c = (i * kWaves + wave) * kSpan;
-    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c, lane, cols - c, 1.f);
+    c[i] = (i * waves + wave) * kSpanCols;
+    in[i].load(a, r, c[i], lane, cols - c[i]);
+    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
+  const int other = lane % kMaxWaves;
+  float mean = a.mean[r], rstd = a.rstd[r];
   int turn = 0;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
-    const float mean = a.mean[r], rstd = a.rstd[r];
-    GradSpan<T, kWave> in[NP];
+  for (; r < a.rows; r += gridDim.x, turn ^= 1) {
+    const int64_t after = r + gridDim.x;
+    const bool more = after < a.rows;
+    if (more) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (i * kWaves + wave) * kSpan;
-      in[i].load(a, r, c, lane, cols - c);
+      for (int i = 0; i < NP; ++i) next[i].load(a, after, c[i], lane, cols - c[i]);
     }
-    float dy[NP][kLanePiece], z[NP][kLanePiece], sh = 0.f, shz = 0.f;
+    const float next_mean = more ? a.mean[after] : 0.f, next_rstd = more ? a.rstd[after] : 0.f;
+    float sh = 0.f, shz = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      in[i].dy.widen_to(dy[i]);
-      in[i].s.widen_to(z[i]);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        z[i][u] = (z[i][u] - mean) * rstd;
-        const float h = dy[i][u] * w[i][u];
-        sh += h;
-        shz += h * z[i][u];
-        gw[i][u] += dy[i][u] * z[i][u];
-        gb[i][u] += dy[i][u];
-      }
-    }
+    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i]);
     sh = wave_sum(sh);
     shz = wave_sum(shz);
     if (lane == 0) {
-      lds[turn][wave] = sh;
-      lds[turn][kWaves + wave] = shz;
+      lds[turn][0][wave] = sh;
+      lds[turn][1][wave] = shz;
     }
     __syncthreads();  // the other half of lds is free again at the next row's
-    float m1 = 0.f, m2 = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      m1 += lds[turn][k];
-      m2 += lds[turn][kWaves + k];
-    }
-    m1 *= inv;
-    m2 *= inv;
+    const float m1 = group_sum<kMaxWaves>(other < waves ? lds[turn][0][other] : 0.f) * inv;
+    const float m2 = group_sum<kMaxWaves>(other < waves ? lds[turn][1][other] : 0.f) * inv;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int c = (i * kWaves + wave) * kSpan;
-      float d[kLanePiece];
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) d[u] = rstd * (dy[i][u] * w[i][u] - m1 - z[i][u] * m2);
-      norm_grad_store<T, kWave>(d, in[i].up, a, drop, n, r, c, lane, cols - c);
+      in[i].finish(w[i], mean, rstd, m1, m2, a, drop, n, r, c[i], lane, cols - c[i]);
+      in[i] = next[i];
     }
+    mean = next_mean;
+    rstd = next_rstd;
   }
   if (part == nullptr) return;
   float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int c = (i * kWaves + wave) * kSpan;
-    Span<T, kWave>::store(mine + c, gw[i], lane, cols - c, false);
-    Span<T, kWave>::store(mine + cols + c, gb[i], lane, cols - c, false);
+    Span<T, kWave>::store(mine + c[i], gw[i], lane, cols - c[i], false);
+    Span<T, kWave>::store(mine + cols + c[i], gb[i], lane, cols - c[i], false);
   }
 }
 
-// Rows of any width: a block reads its row twice (sums, result) and keeps its
-// gradient sums in its row of `part`, each element always by the same thread.
+// Wider rows.  First the rows' two means (m1 and m2, [2][rows] of scratch) ...
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormGradArgs a,
-                                                                     const Drop drop, float* part) {
-  constexpr int kSpan = kWave * kLanePiece;
+__global__ __launch_bounds__(kRowThreads) void norm_grad_means_kernel(const NormGradArgs a,
+                                                                      float* __restrict__ means) {
   __shared__ float lds[2 * kRowWaves];
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t begin = (threadIdx.x >> 6) * kSpan, step = kRowWaves * kSpan;
-  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const int64_t begin = (threadIdx.x >> 6) * kSpanCols, step = kRowWaves * kSpanCols;
   const float inv = 1.f / static_cast<float>(a.cols);
-  float* pw = part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
-  float* pb = pw + a.cols;
-  bool first = true;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sh = 0.f, shz = 0.f;
@@ -590,104 +657,122 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_wide_kernel(const NormG
       }
     }
     block_sum2(sh, shz, lds);
-    const float m1 = sh * inv, m2 = shz * inv;
-    for (int64_t c = begin; c < a.cols; c += step) {
-      const int left = cols_left(c, a.cols);
-      GradSpan<T, kWave> in;
-      float dy[kLanePiece], z[kLanePiece], w[kLanePiece], d[kLanePiece];
-      in.load(a, r, c, lane, left);
-      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
-      in.dy.widen_to(dy);
-      in.s.widen_to(z);
-#pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) {
-        z[u] = (z[u] - mean) * rstd;
-        d[u] = rstd * (dy[u] * w[u] - m1 - z[u] * m2);
-      }
-      norm_grad_store<T, kWave>(d, in.up, a, drop, n, r, c, lane, left);
-      if (part != nullptr) {
-#pragma unroll
-        for (int u = 0; u < kLanePiece; ++u) {
-          const int at = Span<T, kWave>::col(lane, u);
-          if (at < left) {
-            pw[c + at] = (first ? 0.f : pw[c + at]) + dy[u] * z[u];
-            pb[c + at] = (first ? 0.f : pb[c + at]) + dy[u];
-          }
-        }
-      }
+    if (threadIdx.x == 0) {
+      means[r] = sh * inv;
+      means[a.rows + r] = shz * inv;
     }
-    first = false;
   }
 }
+// ... then tiles of columns, a wavefront a span of them: block y takes rows y, y +
+// gridDim.y, ... and keeps its columns' gradient sums in registers.
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void norm_grad_tile_kernel(
+    const NormGradArgs a, const Drop drop, const float* __restrict__ means, float* part) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kRowWaves + (threadIdx.x >> 6)) * kSpanCols;
+  if (c >= a.cols) return;
+  const uint64_t n = drop.t ? drop_offset(drop) : 0;
+  const int left = cols_left(c, a.cols);
+  float w[kLanePiece], gw[kLanePiece], gb[kLanePiece];
+  Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+#pragma unroll
+  for (int u = 0; u < kLanePiece; ++u) gw[u] = gb[u] = 0.f;
+  for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+    GradSpan<T, kWave> in;
+    in.load(a, r, c, lane, left);
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float sh = 0.f, shz = 0.f;
+    in.sums(w, mean, rstd, sh, shz, gw, gb);
+    in.finish(w, mean, rstd, means[r], means[a.rows + r], a, drop, n, r, c, lane, left);
+  }
+  if (part == nullptr) return;
+  float* mine = part + static_cast<int64_t>(blockIdx.y) * 2 * a.cols + c;
+  Span<T, kWave>::store(mine, gw, lane, left, false);
+  Span<T, kWave>::store(mine + a.cols, gb, lane, left, false);
+}
 
-// Sums the blocks' parts: 32 columns a block, 32 threads of partial sums each,
-// joined in order.
-constexpr int kSumCols = 32, kSumThreads = 1024;
-__global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* part, const int blocks,
-                                                                const int64_t cols, float* weight,
-                                                                float* bias) {
-  constexpr int kParts = kSumThreads / kSumCols;
-  __shared__ float lds[kParts][kSumCols + 1];
+// Sums the blocks' parts: 16 columns a block, 64 threads to each, which request
+// 8 parts at a time and add them in order; joined in two steps.
+constexpr int kSumCols = 16, kSumThreads = 1024, kSumAhead = 8;
+__global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* __restrict__ part,
+                                                                const int parts, const int64_t cols,
+                                                                float* __restrict__ weight,
+                                                                float* __restrict__ bias) {
+  constexpr int kGroups = kSumThreads / kSumCols, kJoin = 8;
+  __shared__ float lds[kGroups][kSumCols + 1], joined[kJoin][kSumCols + 1];
   const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + x;
   float v = 0.f;
-  if (i < 2 * cols)
-    for (int k = y; k < blocks; k += kParts) v += part[k * 2 * cols + i];
+  if (i < 2 * cols) {
+    for (int k = y; k < parts; k += kGroups * kSumAhead) {
+      float t[kSumAhead];
+#pragma unroll
+      for (int m = 0; m < kSumAhead; ++m) {
+        const int at = k + m * kGroups;
+        t[m] = at < parts ? part[at * 2 * cols + i] : 0.f;
+      }
+#pragma unroll
+      for (int m = 0; m < kSumAhead; ++m) v += t[m];
+    }
+  }
   lds[y][x] = v;
+  __syncthreads();
+  if (y < kJoin) {
+    v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGroups / kJoin; ++k) v += lds[y * (kGroups / kJoin) + k][x];
+    joined[y][x] = v;
+  }
   __syncthreads();
   if (y != 0 || i >= 2 * cols) return;
   float* out = i < cols ? weight : bias;
   if (out == nullptr) return;
   v = 0.f;
 #pragma unroll
-  for (int k = 0; k < kParts; ++k) v += lds[k][x];
+  for (int k = 0; k < kJoin; ++k) v += joined[k][x];
   out[i < cols ? i : i - cols] = v;
 }
 
-// Form of the backward's rows and its blocks: 4 of 256 threads to a CU, fewer
-// where the parts would exceed 64 MB.
-struct GradForm {
-  int threads;   // of a block
-  int lanes;     // of a row (threads: a block a row)
-  int pieces;    // of a lane; 0: the wide kernel
-};
-static GradForm grad_form(int64_t cols) {
-  const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
-  if (n <= 64) {
-    int g = 1;
-    while (g < n) g *= 2;
-    return {kRowThreads, g, 1};
-  }
-  if (n <= 128) return {kRowThreads, kWave, 2};
-  if (n <= 256) return {256, 256, 1};
-  if (n <= 512) return {256, 256, 2};
-  if (n <= 1024) return {512, 512, 2};
-  if (n <= 2048) return {1024, 1024, 2};
-  return {kRowThreads, kRowThreads, 0};
-}
-static int norm_grad_blocks(int64_t rows, int64_t cols) {
-  const GradForm f = grad_form(cols);
-  const int per_block = f.threads / f.lanes;
-  const int64_t most = (int64_t{1} << 23) / cols;
-  int64_t n = (rows + per_block - 1) / per_block;
-  const int64_t fill = int64_t{4} * 256 * kRowThreads / f.threads;
-  n = n < fill ? n : fill;
-  return static_cast<int>(n < most ? n : (most < 1 ? 1 : most));
+// One span a lane takes up to 128 registers, two up to 256.
+static RowForm grad_form(int64_t cols) { return row_form(cols, 16, 8, kMaxWaves); }
+
+// Rows of `part`: blocks that walk rows; of the wide form, the blocks that
+// share a tile of columns (8 blocks to a CU over all tiles).
+static int norm_grad_parts(int64_t rows, int64_t cols) {
+  const RowForm f = grad_form(cols);
+  if (f.spans != 0) return static_cast<int>(row_blocks(f, rows));
+  const int64_t tiles = (cols + kRowWaves * kSpanCols - 1) / (kRowWaves * kSpanCols);
+  const int64_t want = tiles < 2048 ? 2048 / tiles : 1;
+  return static_cast<int>(rows < want ? rows : want);
 }
 
-size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols) {
-  return static_cast<size_t>(norm_grad_blocks(rows, cols)) * 2 * cols * sizeof(float);
+size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols, bool sums) {
+  const size_t part = sums ? static_cast<size_t>(norm_grad_parts(rows, cols)) * 2 * cols : 0;
+  return (part + (grad_form(cols).spans == 0 ? 2 * static_cast<size_t>(rows) : 0)) * sizeof(float);
 }
 
 template <typename T>
-static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, int blocks,
-                               hipStream_t stream) {
-  const GradForm f = grad_form(a.cols);
-  const dim3 grid(blocks), block(f.threads);
+static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, float* means,
+                               int parts, hipStream_t stream) {
+  const RowForm f = grad_form(a.cols);
+  const dim3 grid(parts), block(f.lanes <= kWave ? kRowThreads : f.lanes);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop, part);
   };
-  switch (f.pieces == 0 ? 0 : f.lanes * f.pieces) {
+  if (f.spans == 0) {
+    const int64_t most = 2048;
+    hipLaunchKernelGGL(norm_grad_means_kernel<T>,
+                       dim3(static_cast<uint32_t>(a.rows < most ? a.rows : most)), block, 0, stream,
+                       a, means);
+    const int64_t tiles = (a.cols + kRowWaves * kSpanCols - 1) / (kRowWaves * kSpanCols);
+    hipLaunchKernelGGL(norm_grad_tile_kernel<T>, dim3(static_cast<uint32_t>(tiles), parts), block, 0,
+                       stream, a, drop, means, part);
+    return;
+  }
+  if (f.lanes > kWave)
+    return f.spans == 1 ? launch(norm_grad_block_kernel<T, 1024, 1>)
+                        : launch(norm_grad_block_kernel<T, 512, 2>);
+  switch (f.lanes * f.spans) {
     case 1: return launch(norm_grad_group_kernel<T, 1, 1>);
     case 2: return launch(norm_grad_group_kernel<T, 2, 1>);
     case 4: return launch(norm_grad_group_kernel<T, 4, 1>);
@@ -695,12 +780,7 @@ static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* p
     case 16: return launch(norm_grad_group_kernel<T, 16, 1>);
     case 32: return launch(norm_grad_group_kernel<T, 32, 1>);
     case 64: return launch(norm_grad_group_kernel<T, 64, 1>);
-    case 128: return launch(norm_grad_group_kernel<T, 64, 2>);
-    case 256: return launch(norm_grad_block_kernel<T, 256, 1>);
-    case 512: return launch(norm_grad_block_kernel<T, 256, 2>);
-    case 1024: return launch(norm_grad_block_kernel<T, 512, 2>);
-    case 2048: return launch(norm_grad_block_kernel<T, 1024, 2>);
-    default: return launch(norm_grad_wide_kernel<T>);
+    default: return launch(norm_grad_group_kernel<T, 64, 2>);
   }
 }
 
@@ -709,17 +789,18 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& dro
   NormGradArgs a = args;
   a.stream = streams(bf16, a.rows, a.cols);
   const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
-  const int blocks = norm_grad_blocks(a.rows, a.cols);
+  const int parts = norm_grad_parts(a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;
+  float* means = static_cast<float*>(workspace) + (sums ? static_cast<size_t>(parts) * 2 * a.cols : 0);
   if (bf16)
-    launch_norm_grad_t<uint16_t>(a, drop, part, blocks, stream);
+    launch_norm_grad_t<uint16_t>(a, drop, part, means, parts, stream);
   else
-    launch_norm_grad_t<float>(a, drop, part, blocks, stream);
+    launch_norm_grad_t<float>(a, drop, part, means, parts, stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums) {
     hipLaunchKernelGGL(sum_parts_kernel,
                        dim3(static_cast<uint32_t>((2 * a.cols + kSumCols - 1) / kSumCols)),
-                       dim3(kSumThreads), 0, stream, part, blocks, a.cols, a.grad_weight,
+                       dim3(kSumThreads), 0, stream, part, parts, a.cols, a.grad_weight,
                        a.grad_bias);
     e = hipGetLastError();
   }

@@ -221,6 +221,16 @@ struct Span {
       q[i] = load_vec(p + c, left - c);
     }
   }
+  // From here on the compiler takes the span as new: values made from it before
+  // are made again rather than kept in registers.
+  __device__ __forceinline__ void renew() {
+    static_assert(sizeof(q) % 4 == 0, "whole registers");
+    uint32_t word[sizeof(q) / 4];
+    __builtin_memcpy(word, q, sizeof(q));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(q) / 4; ++i) asm("" : "+v"(word[i]));
+    __builtin_memcpy(q, word, sizeof(q));
+  }
   __device__ __forceinline__ void widen_to(float v[kLanePiece]) const {
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) v[u] = widen(q[u / kVec<T>][u % kVec<T>]);
@@ -325,9 +335,9 @@ __device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v);
 hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, const RowsOut& out,
                           int64_t rows, int64_t cols, const Drop& drop, hipStream_t stream);
 hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream);
-// workspace: norm_grad_workspace_bytes, null when neither weight nor bias gradient
+// workspace: norm_grad_workspace_bytes (may be 0); sums: a weight or bias gradient
 // is wanted.
-size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols);
+size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols, bool sums);
 hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, void* workspace,
                             hipStream_t stream);
 

@@ -31,14 +31,15 @@ __device__ __forceinline__ int keys_left(int64_t k, int64_t K) { return static_c
 template <typename T>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
                                                                 const BucketMap map, const int tx,
-                                                                const uint32_t tiles) {
+                                                                const uint32_t k_tiles,
+                                                                const uint32_t per) {
   constexpr int V = kVec<T>;
   __shared__ int32_t borders[kMaxBuckets];
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
-  const int64_t k = (static_cast<int64_t>(blockIdx.x % tiles) * tx + x) * V;
-  const uint32_t row = blockIdx.x / tiles * (kBiasThreads / tx) + y;
+  const int64_t k = (static_cast<int64_t>(blockIdx.x % k_tiles) * tx + x) * V;
+  const uint32_t row = tile_of(per, k_tiles) * (kBiasThreads / tx) + y;
   if (k >= a.K || row >= static_cast<uint32_t>(a.B * a.H * a.Q)) return;
   const uint32_t bh = row / static_cast<uint32_t>(a.Q), q = row - bh * static_cast<uint32_t>(a.Q);
   const uint32_t b = bh / static_cast<uint32_t>(a.H), h = bh - b * static_cast<uint32_t>(a.H);
@@ -75,47 +76,81 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
 // key - query alone: a block writes the table's entries for the tile's
 // differences to LDS once (tile's keys + queries of them, not keys x queries),
 // and a lane reads for 8 queries and its keys the few that they take (8 keys: 15).
+// The first scores are on their way meanwhile.  Short sequences: a block takes
+// several (batch, head) pairs, a window of differences to each.
 // ---------------------------------------------------------------------------
 constexpr int kStep = 8;      // queries a lane takes at a time
 constexpr int kMaxSteps = 4;
 
+struct BiasTile {
+  int steps;         // a group's, of 8 queries each
+  uint32_t pairs;    // (batch, head) pairs of a block
+  uint32_t groups;   // of lanes to a pair
+  uint32_t q_tiles;  // of a pair
+  uint32_t k_tiles;
+  uint32_t per;      // tile_of
+};
+
 template <typename T, int TX>
 __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs a,
                                                                  const BucketMap map,
-                                                                 const int steps,
-                                                                 const int64_t q_tiles,
-                                                                 const int64_t k_tiles) {
+                                                                 const BiasTile tl) {
   constexpr int V = kVec<T>, TY = kBiasThreads / TX, kKeys = TX * V;
+  constexpr int kOne = kKeys + kMaxSteps * TY * kStep, kMany = TY * (kKeys + kStep);
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float column[kMaxBuckets];
-  __shared__ float window[kKeys + kMaxSteps * TY * kStep];
-  const int64_t blk = blockIdx.x;
-  const int64_t kt = blk % k_tiles, qt = blk / k_tiles % q_tiles, bh = blk / (k_tiles * q_tiles);
-  const int64_t b = bh / a.H, h = bh - b * a.H;
+  __shared__ float windows[kOne > kMany ? kOne : kMany];
+  const uint32_t tile = tile_of(tl.per, tl.k_tiles), kt = blockIdx.x % tl.k_tiles;
+  const uint32_t pt = tile / tl.q_tiles, qt = tile - pt * tl.q_tiles;
+  const uint32_t H = static_cast<uint32_t>(a.H), all = static_cast<uint32_t>(a.B * a.H);
+  const uint32_t bh0 = pt * tl.pairs;
+  if (bh0 >= all) return;
+  const int rows = tl.steps * static_cast<int>(tl.groups) * kStep;  // of a pair's tile
+  const int64_t q0 = static_cast<int64_t>(qt) * rows, k0 = static_cast<int64_t>(kt) * kKeys;
+  const int x = threadIdx.x % TX;
+  const uint32_t y = threadIdx.x / TX;
+  const uint32_t pair = tl.pairs == 1 ? 0 : y / tl.groups;
+  const uint32_t bh = bh0 + pair, b = bh / H, h = bh - b * H;
+  const bool mine = pair < tl.pairs && bh < all;
+  const int64_t k = k0 + x * V;
+  const int len = mine ? keys_left(k, a.K) : 0;
+  int row = static_cast<int>(y - pair * tl.groups) * kStep;
+  const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
+  typename Vec<T>::type raw[kStep];
+  if (a.in != nullptr) {
+#pragma unroll
+    for (int j = 0; j < kStep; ++j)
+      raw[j] = load_vec(in + (q0 + row + j) * a.in_stride[2], q0 + row + j < a.Q ? len : 0);
+  }
   for (int i = threadIdx.x; i < map.num; i += kBiasThreads) {
     if (i < map.side) borders[i] = map.borders[i];
-    column[i] = table_entry(a, i * a.H + h);
+    if (tl.pairs == 1) column[i] = table_entry(a, static_cast<int64_t>(i) * a.H + h);
   }
-  const int rows = steps * TY * kStep;  // of the tile
-  const int64_t q0 = qt * rows, k0 = kt * kKeys;
-  // difference of window[0]: the tile's first key, its last query
-  const int32_t rel0 = static_cast<int32_t>(k0 - q0 - (rows - 1)) - first_position(a, b);
   __syncthreads();
-  for (int i = threadIdx.x; i < kKeys + rows - 1; i += kBiasThreads)
-    window[i] = column[bucket_of(rel0 + i, borders, map.side, map.both)];
+  const int size = kKeys + rows;  // of a window, with one more than it needs
+  // difference of its first entry: the tile's first key, its last query
+  const int32_t rel0 = static_cast<int32_t>(k0 - q0 - (rows - 1));
+  if (tl.pairs == 1) {
+    const int32_t rel = rel0 - first_position(a, b);
+    for (int i = threadIdx.x; i < size - 1; i += kBiasThreads)
+      windows[i] = column[bucket_of(rel + i, borders, map.side, map.both)];
+  } else {
+    for (uint32_t i = threadIdx.x; i < tl.pairs * size; i += kBiasThreads) {
+      const uint32_t w = i / size, bh1 = bh0 + w, b1 = bh1 / H;
+      if (bh1 >= all) break;
+      const int32_t rel = rel0 - first_position(a, b1) + static_cast<int32_t>(i - w * size);
+      windows[i] = table_entry(
+          a, static_cast<int64_t>(bucket_of(rel, borders, map.side, map.both)) * a.H + bh1 - b1 * H);
+    }
+  }
   __syncthreads();
-  const int x = threadIdx.x % TX, y = threadIdx.x / TX;
-  const int64_t k = k0 + x * V;
-  if (k >= a.K) return;
-  const int len = keys_left(k, a.K);
-  const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
+  if (len <= 0) return;
+  const float* window = windows + pair * size;
   T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] + k;
-  for (int s = 0; s < steps; ++s) {
-    const int row = (s * TY + y) * kStep;
+  for (int s = 0; s < tl.steps; ++s, row += static_cast<int>(tl.groups) * kStep) {
     const int64_t q = q0 + row;
     if (q >= a.Q) return;
-    typename Vec<T>::type raw[kStep];
-    if (a.in != nullptr) {
+    if (a.in != nullptr && s > 0) {
 #pragma unroll
       for (int j = 0; j < kStep; ++j)
         if (q + j < a.Q) raw[j] = load_vec(in + (q + j) * a.in_stride[2], len);
@@ -139,11 +174,11 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
   }
 }
 
-// Lanes along the keys, `vec` keys each: as many as there are keys, 16 to a whole
-// block.
-static int key_lanes(int64_t K, int vec) {
+// Lanes along the keys, `vec` keys each: as many as there are keys, `least` to a
+// whole block.
+static int key_lanes(int64_t K, int vec, int least) {
   const int64_t pieces = (K + vec - 1) / vec;
-  int tx = 16;
+  int tx = least;
   while (tx < pieces && tx < kBiasThreads) tx *= 2;
   return tx;
 }
@@ -151,28 +186,48 @@ static int key_lanes(int64_t K, int vec) {
 template <typename T>
 static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
   const dim3 block(kBiasThreads);
-  const int tx = key_lanes(a.K, kVec<T>), ty = kBiasThreads / tx;
+  const int tx = key_lanes(a.K, kVec<T>, 4), ty = kBiasThreads / tx;
   const int64_t keys = static_cast<int64_t>(tx) * kVec<T>;
   const int64_t k_tiles = (a.K + keys - 1) / keys, bh = a.B * a.H;
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
     const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
-    if (row_tiles > INT32_MAX / k_tiles) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(bias_row_kernel<T>, dim3(static_cast<uint32_t>(row_tiles * k_tiles)), block, 0,
-                       stream, a, map, tx, static_cast<uint32_t>(k_tiles));
+    const TileGrid tg = tile_grid(row_tiles, k_tiles);
+    if (!tg.fits) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(bias_row_kernel<T>, tg.grid, block, 0, stream, a, map, tx,
+                       static_cast<uint32_t>(k_tiles), tg.per);
     return hipGetLastError();
   }
-  // as many queries to a block as leave 8 blocks to a CU
-  int steps = kMaxSteps;
-  while (steps > 1 && bh * k_tiles * ((a.Q + ty * kStep * steps - 1) / (ty * kStep * steps)) < 2048)
-    steps /= 2;
-  const int64_t q_tiles = (a.Q + ty * kStep * steps - 1) / (ty * kStep * steps);
-  if (bh > INT32_MAX / q_tiles / k_tiles) return hipErrorInvalidConfiguration;
-  const dim3 grid(static_cast<uint32_t>(bh * q_tiles * k_tiles));
+  BiasTile tl;
+  tl.steps = 1;
+  tl.pairs = 1;
+  tl.groups = ty;
+  int64_t q_tiles = 1;
+  const int64_t q_steps = (a.Q + kStep - 1) / kStep;
+  if (k_tiles == 1 && 2 * q_steps <= ty) {
+    tl.groups = static_cast<uint32_t>(q_steps);
+    tl.pairs = ty / tl.groups;
+    while (tl.pairs > 1 && bh < 2048 * static_cast<int64_t>(tl.pairs)) tl.pairs /= 2;
+  } else {
+    // as many queries to a block as leave 8 blocks to a CU
+    tl.steps = kMaxSteps;
+    while (tl.steps > 1 && bh * k_tiles * ((q_steps + ty * tl.steps - 1) / (ty * tl.steps)) < 2048)
+      tl.steps /= 2;
+    q_tiles = (q_steps + ty * tl.steps - 1) / (ty * tl.steps);
+  }
+  const int64_t tiles = (bh + tl.pairs - 1) / tl.pairs * q_tiles;
+  const TileGrid tg = tile_grid(tiles, k_tiles);
+  // (tile_of of a slice past the end stays below 2^32 too)
+  if (!tg.fits || tiles > INT32_MAX) return hipErrorInvalidConfiguration;
+  tl.q_tiles = static_cast<uint32_t>(q_tiles);
+  tl.k_tiles = static_cast<uint32_t>(k_tiles);
+  tl.per = tg.per;
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, map, steps, q_tiles, k_tiles);
+    hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, tl);
     return hipGetLastError();
   };
   switch (tx) {
+    case 4: return launch(bias_tile_kernel<T, 4>);
+    case 8: return launch(bias_tile_kernel<T, 8>);
     case 16: return launch(bias_tile_kernel<T, 16>);
     case 32: return launch(bias_tile_kernel<T, 32>);
     case 64: return launch(bias_tile_kernel<T, 64>);
@@ -397,7 +452,7 @@ struct FarShape {
 static FarShape far_shape(bool bf16, const BiasArgs& a) {
   FarShape s;
   const int vec = bf16 ? kVec<uint16_t> : kVec<float>;
-  s.tx = key_lanes(a.K, vec);
+  s.tx = key_lanes(a.K, vec, 16);
   if (s.tx > kWave) s.tx = kWave;
   const int groups = kBiasThreads / s.tx;
   const int64_t keys = static_cast<int64_t>(s.tx) * vec;
@@ -414,15 +469,16 @@ static FarShape far_shape(bool bf16, const BiasArgs& a) {
 template <typename T, int TX>
 __global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(
     const BiasArgs a, const BucketMap map, const int rows, const int64_t q_tiles,
-    const int64_t k_tiles, float* __restrict__ part) {
+    const int64_t k_tiles, const uint32_t per, float* __restrict__ part) {
   constexpr int V = kVec<T>, kGroups = kBiasThreads / TX, kKeys = TX * V;
   constexpr int kWaveGroups = kWave / TX, kDiagonals = V + kStep - 1;
   __shared__ float windows[kGroups][kKeys + kMaxGradRows];
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float sums[kBiasWaves][kMaxBuckets];
-  const int64_t blk = blockIdx.x;
+  const uint32_t blk = tile_of(per, 1);
   const int64_t kt = blk % k_tiles, qt = blk / k_tiles % q_tiles, bh = blk / (k_tiles * q_tiles);
   const int64_t b = bh / a.H, h = bh - b * a.H;
+  if (b >= a.B) return;
   const int x = threadIdx.x % TX, group = threadIdx.x / TX;
   for (int i = x; i < kKeys + kMaxGradRows; i += TX) windows[group][i] = 0.f;
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
@@ -538,9 +594,10 @@ static void launch_near(const BiasArgs& a, const BucketMap& map, const NearShape
 template <typename T>
 static void launch_far(const BiasArgs& a, const BucketMap& map, const FarShape& s, float* part,
                        hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(a.B * a.H * s.q_tiles * s.k_tiles)), block(kBiasThreads);
+  const TileGrid tg = tile_grid(a.B * a.H * s.q_tiles * s.k_tiles, 1);  // (bias_grad_fits)
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, map, s.rows, s.q_tiles, s.k_tiles, part);
+    hipLaunchKernelGGL(kernel, tg.grid, dim3(kBiasThreads), 0, stream, a, map, s.rows, s.q_tiles,
+                       s.k_tiles, tg.per, part);
   };
   switch (s.tx) {
     case 16: return launch(bias_grad_far_kernel<T, 16>);

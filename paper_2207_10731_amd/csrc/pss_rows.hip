@@ -29,11 +29,12 @@ template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, const RowsIn residual,
                                                               const RowsOut out, const int64_t rows,
                                                               const int64_t cols,
-                                                              const uint32_t spans, const Drop drop,
+                                                              const uint32_t spans,
+                                                              const uint32_t per, const Drop drop,
                                                               const bool stream) {
   typedef Span<T, G> S;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
-  const uint32_t tile = blockIdx.x / spans, span = blockIdx.x - tile * spans;
+  const uint32_t tile = tile_of(per, spans), span = blockIdx.x % spans;
   const int lane = threadIdx.x % G;
   const int64_t r = static_cast<int64_t>(tile) * (kRowThreads / G) + threadIdx.x / G;
   const int64_t c = static_cast<int64_t>(span) * (G * kLanePiece);
@@ -68,10 +69,11 @@ static hipError_t launch_dropout_t(const RowsIn& x, const RowsIn& residual, cons
   const int g = row_lanes(cols);
   const int64_t spans = (cols + g * kLanePiece - 1) / (g * kLanePiece);
   const int64_t tiles = (rows * g + kRowThreads - 1) / kRowThreads;
-  if (tiles > INT32_MAX / spans) return hipErrorInvalidConfiguration;
+  const TileGrid tg = tile_grid(tiles, spans);
+  if (!tg.fits) return hipErrorInvalidConfiguration;
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * spans)), dim3(kRowThreads), 0,
-                       stream, x, residual, out, rows, cols, static_cast<uint32_t>(spans), drop,
+    hipLaunchKernelGGL(kernel, tg.grid, dim3(kRowThreads), 0, stream, x, residual, out, rows, cols,
+                       static_cast<uint32_t>(spans), tg.per, drop,
                        streams(sizeof(T) == 2, rows, cols));
     return hipGetLastError();
   };
@@ -325,8 +327,10 @@ __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArg
       float v[kLanePiece];
       in.load(a, r, c, lane, cols_left(c, a.cols));
       in.sum_to(v, a, drop, n, r, c, lane);
+      float piece = 0.f;  // of its own: a long row's chain of additions is 8 times shorter
 #pragma unroll
-      for (int u = 0; u < kLanePiece; ++u) sum += v[u];
+      for (int u = 0; u < kLanePiece; ++u) piece += v[u];
+      sum += piece;
     }
     block_sum2(sum, zero, lds);
     const float mean = sum * inv;
@@ -649,12 +653,15 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_means_kernel(const Norm
       Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
       g.widen_to(dy);
       s.widen_to(z);
+      float ph = 0.f, phz = 0.f;
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) {
         const float h = dy[u] * w[u];
-        sh += h;
-        shz += h * ((z[u] - mean) * rstd);
+        ph += h;
+        phz += h * ((z[u] - mean) * rstd);
       }
+      sh += ph;
+      shz += phz;
     }
     block_sum2(sh, shz, lds);
     if (threadIdx.x == 0) {
@@ -701,36 +708,39 @@ __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* __r
   constexpr int kGroups = kSumThreads / kSumCols, kJoin = 8;
   __shared__ float lds[kGroups][kSumCols + 1], joined[kJoin][kSumCols + 1];
   const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + x;
-  float v = 0.f;
-  if (i < 2 * cols) {
-    for (int k = y; k < parts; k += kGroups * kSumAhead) {
-      float t[kSumAhead];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kSumCols;
+  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kSumCols; i0 < 2 * cols; i0 += step) {
+    const int64_t i = i0 + x;
+    float v = 0.f;
+    if (i < 2 * cols) {
+      for (int k = y; k < parts; k += kGroups * kSumAhead) {
+        float t[kSumAhead];
 #pragma unroll
-      for (int m = 0; m < kSumAhead; ++m) {
-        const int at = k + m * kGroups;
-        t[m] = at < parts ? part[at * 2 * cols + i] : 0.f;
+        for (int m = 0; m < kSumAhead; ++m) {
+          const int at = k + m * kGroups;
+          t[m] = at < parts ? part[at * 2 * cols + i] : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < kSumAhead; ++m) v += t[m];
       }
+    }
+    lds[y][x] = v;
+    __syncthreads();
+    if (y < kJoin) {
+      v = 0.f;
 #pragma unroll
-      for (int m = 0; m < kSumAhead; ++m) v += t[m];
+      for (int k = 0; k < kGroups / kJoin; ++k) v += lds[y * (kGroups / kJoin) + k][x];
+      joined[y][x] = v;
+    }
+    __syncthreads();
+    float* out = i < cols ? weight : bias;
+    if (y == 0 && i < 2 * cols && out != nullptr) {
+      v = 0.f;
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) v += joined[k][x];
+      out[i < cols ? i : i - cols] = v;
     }
   }
-  lds[y][x] = v;
-  __syncthreads();
-  if (y < kJoin) {
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kGroups / kJoin; ++k) v += lds[y * (kGroups / kJoin) + k][x];
-    joined[y][x] = v;
-  }
-  __syncthreads();
-  if (y != 0 || i >= 2 * cols) return;
-  float* out = i < cols ? weight : bias;
-  if (out == nullptr) return;
-  v = 0.f;
-#pragma unroll
-  for (int k = 0; k < kJoin; ++k) v += joined[k][x];
-  out[i < cols ? i : i - cols] = v;
 }
 
 // One span a lane takes up to 128 registers, two up to 256.
@@ -798,8 +808,9 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& dro
     launch_norm_grad_t<float>(a, drop, part, means, parts, stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums) {
+    const int64_t blocks = (2 * a.cols + kSumCols - 1) / kSumCols;
     hipLaunchKernelGGL(sum_parts_kernel,
-                       dim3(static_cast<uint32_t>((2 * a.cols + kSumCols - 1) / kSumCols)),
+                       dim3(static_cast<uint32_t>(blocks < kGridBlocks ? blocks : kGridBlocks - 1)),
                        dim3(kSumThreads), 0, stream, part, parts, a.cols, a.grad_weight,
                        a.grad_bias);
     e = hipGetLastError();

@@ -328,6 +328,31 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
 
+// Workgroups in one dimension of a grid: it holds fewer than 2^32 work-items
+// (a larger one is cut to its low 32 bits without an error).
+constexpr int64_t kGridBlocks = 1 << 22;  // of up to 1024 threads less one
+constexpr int64_t kGridSlices = 65535;    // of the second dimension
+
+// tiles x parts workgroups: grid.x holds `per` tiles of `parts` each, grid.y as many
+// such slices as it takes (tile_of; the last slice may lie past the end).
+struct TileGrid {
+  dim3 grid;
+  uint32_t per = 0;
+  bool fits = false;
+};
+inline TileGrid tile_grid(int64_t tiles, int64_t parts) {
+  TileGrid g;
+  const int64_t most = parts < kGridBlocks ? (kGridBlocks - 1) / parts : 1;
+  const int64_t per = tiles < most ? tiles : most, slices = (tiles + per - 1) / per;
+  g.fits = parts < kGridBlocks && slices <= kGridSlices;
+  g.grid = dim3(static_cast<uint32_t>(per * parts), static_cast<uint32_t>(slices));
+  g.per = static_cast<uint32_t>(per);
+  return g;
+}
+__device__ __forceinline__ uint32_t tile_of(uint32_t per, uint32_t parts) {
+  return blockIdx.y * per + blockIdx.x / parts;
+}
+
 // Host-side launchers.
 //
 // Operators on rows (pss_rows.hip) of float32 or bfloat16 elements; rows,

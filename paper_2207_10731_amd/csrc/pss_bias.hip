@@ -1,5 +1,7 @@
 // Learned relative position bias by buckets: scores + table[bucket], and the
 // table's gradient.
+#include <type_traits>
+
 #include "pss_rows.hpp"
 
 namespace pss {
@@ -22,19 +24,26 @@ __device__ __forceinline__ float table_entry(const BiasArgs& a, int64_t i) {
 }
 // Keys from k on, as an int; a lane takes 16 bytes of them at a time (kVec).
 __device__ __forceinline__ int keys_left(int64_t k, int64_t K) { return static_cast<int>(K - k); }
+// Elements of a row's last vector.
+template <typename T>
+__device__ __forceinline__ int key_rest(int64_t K) {
+  return static_cast<int>(K) & (kVec<T> - 1);
+}
 
 // ---------------------------------------------------------------------------
 // Forward, few queries (new tokens): 16 bytes of keys a lane.  Buckets are
 // ranges of distances, so keys whose ends share one (nearly all of a long cache)
 // need two searches, not one each.
 // ---------------------------------------------------------------------------
-template <typename T>
+template <typename T, bool ENDS>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
                                                                 const BucketMap map, const int tx,
                                                                 const uint32_t k_tiles,
                                                                 const uint32_t per) {
   constexpr int V = kVec<T>;
+  constexpr End kEnd = ENDS ? End::kPieces : End::kWhole;
   __shared__ int32_t borders[kMaxBuckets];
+  const int rest = key_rest<T>(a.K);
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
@@ -47,8 +56,8 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
   float v[V];
   typename Vec<T>::type raw;
   if (a.in != nullptr)
-    raw = load_vec(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
-                        q * a.in_stride[2] + k, len);
+    raw = load_vec<kEnd>(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
+                             q * a.in_stride[2] + k, len, rest);
   const int32_t rel = static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q);
   const int j0 = bucket_of(rel, borders, map.side, map.both);
   const int j1 = bucket_of(rel + V - 1, borders, map.side, map.both);
@@ -64,11 +73,12 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
       v[u] = table_entry(a, bucket_of(rel + u, borders, map.side, map.both) * a.H + h);
   }
   if (a.in != nullptr) {
+    raw = settle<kEnd>(raw, len, rest);
 #pragma unroll
     for (int u = 0; u < V; ++u) v[u] += widen(raw[u]);
   }
-  store_vec(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
-                q * a.out_stride[2] + k, v, len, a.stream);
+  store_vec<ENDS>(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
+                      q * a.out_stride[2] + k, v, len, a.stream);
 }
 
 // ---------------------------------------------------------------------------
@@ -91,7 +101,7 @@ struct BiasTile {
   uint32_t per;      // tile_of
 };
 
-template <typename T, int TX>
+template <typename T, int TX, End E>
 __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs a,
                                                                  const BucketMap map,
                                                                  const BiasTile tl) {
@@ -114,13 +124,14 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
   const bool mine = pair < tl.pairs && bh < all;
   const int64_t k = k0 + x * V;
   const int len = mine ? keys_left(k, a.K) : 0;
+  const int rest = key_rest<T>(a.K);
   int row = static_cast<int>(y - pair * tl.groups) * kStep;
   const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
   typename Vec<T>::type raw[kStep];
   if (a.in != nullptr) {
 #pragma unroll
     for (int j = 0; j < kStep; ++j)
-      raw[j] = load_vec(in + (q0 + row + j) * a.in_stride[2], q0 + row + j < a.Q ? len : 0);
+      raw[j] = load_vec<E>(in + (q0 + row + j) * a.in_stride[2], q0 + row + j < a.Q ? len : 0, rest);
   }
   for (int i = threadIdx.x; i < map.num; i += kBiasThreads) {
     if (i < map.side) borders[i] = map.borders[i];
@@ -153,7 +164,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
     if (a.in != nullptr && s > 0) {
 #pragma unroll
       for (int j = 0; j < kStep; ++j)
-        if (q + j < a.Q) raw[j] = load_vec(in + (q + j) * a.in_stride[2], len);
+        if (q + j < a.Q) raw[j] = load_vec<E>(in + (q + j) * a.in_stride[2], len, rest);
     }
     // bias of query q + j and key k + u: near[7 + u - j]
     const int at = x * V + rows - 1 - row - (kStep - 1);
@@ -164,12 +175,13 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
     for (int j = 0; j < kStep; ++j) {
       if (q + j >= a.Q) break;
       float v[V];
+      if (a.in != nullptr) raw[j] = settle<E>(raw[j], len, rest);
 #pragma unroll
       for (int u = 0; u < V; ++u) {
         v[u] = near[kStep - 1 + u - j];
         if (a.in != nullptr) v[u] += widen(raw[j][u]);
       }
-      store_vec(out + (q + j) * a.out_stride[2], v, len, a.stream);
+      store_vec<E != End::kWhole>(out + (q + j) * a.out_stride[2], v, len, a.stream);
     }
   }
 }
@@ -183,6 +195,15 @@ static int key_lanes(int64_t K, int vec, int least) {
   return tx;
 }
 
+// f(the constant that n equals); n is one of them.
+template <int N, int... MORE, typename F>
+static auto with_lanes(int n, F f) {
+  if constexpr (sizeof...(MORE) > 0) {
+    if (n != N) return with_lanes<MORE...>(n, f);
+  }
+  return f(std::integral_constant<int, N>{});
+}
+
 template <typename T>
 static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
   const dim3 block(kBiasThreads);
@@ -193,9 +214,12 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
     const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
     const TileGrid tg = tile_grid(row_tiles, k_tiles);
     if (!tg.fits) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(bias_row_kernel<T>, tg.grid, block, 0, stream, a, map, tx,
-                       static_cast<uint32_t>(k_tiles), tg.per);
-    return hipGetLastError();
+    const auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, tx,
+                         static_cast<uint32_t>(k_tiles), tg.per);
+      return hipGetLastError();
+    };
+    return a.K % kVec<T> ? launch(bias_row_kernel<T, true>) : launch(bias_row_kernel<T, false>);
   }
   BiasTile tl;
   tl.steps = 1;
@@ -225,15 +249,16 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
     hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, tl);
     return hipGetLastError();
   };
-  switch (tx) {
-    case 4: return launch(bias_tile_kernel<T, 4>);
-    case 8: return launch(bias_tile_kernel<T, 8>);
-    case 16: return launch(bias_tile_kernel<T, 16>);
-    case 32: return launch(bias_tile_kernel<T, 32>);
-    case 64: return launch(bias_tile_kernel<T, 64>);
-    case 128: return launch(bias_tile_kernel<T, 128>);
-    default: return launch(bias_tile_kernel<T, 256>);
-  }
+  return with_lanes<4, 8, 16, 32, 64, 128, 256>(tx, [&](auto lanes) {
+    constexpr int TX = lanes.value;
+    if (a.K % kVec<T> == 0) return launch(bias_tile_kernel<T, TX, End::kWhole>);
+    // the lane with a row's end has the elements before it in its own wavefront,
+    // unless it is the first one
+    if (a.K / kVec<T> % (TX < kWave ? TX : kWave) != 0)
+      return launch(bias_tile_kernel<T, TX, End::kOverlap>);
+    if constexpr (TX == 4 || TX >= kWave) return launch(bias_tile_kernel<T, TX, End::kPieces>);
+    return hipErrorInvalidValue;  // not reached: TX of 8 to 32 has more than TX / 2 vectors
+  });
 }
 
 // Results of more than this are stored past the caches.
@@ -327,7 +352,7 @@ static NearShape near_shape(bool bf16, const BiasArgs& a, const BucketMap& map) 
   return s;
 }
 
-template <typename T, int TX, int QU>
+template <typename T, int TX, int QU, End E>
 __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
     const BiasArgs a, const BucketMap map, const uint32_t q_steps, const uint32_t k_steps,
     const int64_t units, const int window, float* __restrict__ part) {
@@ -355,6 +380,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
   uint32_t row = static_cast<uint32_t>(unit / k_steps);
   uint32_t kt = static_cast<uint32_t>(unit - static_cast<int64_t>(row) * k_steps);
   const uint32_t rows = static_cast<uint32_t>(a.B) * q_steps;
+  const int rest = key_rest<T>(a.K);
   float behind_sum = 0.f, ahead_sum = 0.f;
   for (; unit < end; ++unit) {
     const uint32_t r = row * kGroups + group;  // this group's step
@@ -370,7 +396,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
       const int len = keys_left(k0 + c * (TX * V), a.K);
 #pragma unroll
       for (int j = 0; j < QU; ++j)
-        raw[c][j] = load_vec(in + j * a.in_stride[2] + c * (TX * V), j < left ? len : 0);
+        raw[c][j] = load_vec<E>(in + j * a.in_stride[2] + c * (TX * V), j < left ? len : 0, rest);
     }
     const int32_t pos = (left > 0 ? first_position(a, b) : 0) + static_cast<int32_t>(q);
 #pragma unroll
@@ -385,6 +411,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
       for (int i = 0; i < V + QU - 1; ++i) diag[i] = 0.f;
 #pragma unroll
       for (int j = 0; j < QU; ++j) {
+        raw[c][j] = settle<E>(raw[c][j], j < left ? keys_left(k, a.K) : 0, rest);
 #pragma unroll
         for (int u = 0; u < V; ++u) diag[QU - 1 + u - j] += widen(raw[c][j][u]);
       }
@@ -466,7 +493,7 @@ static FarShape far_shape(bool bf16, const BiasArgs& a) {
   return s;
 }
 
-template <typename T, int TX>
+template <typename T, int TX, End E>
 __global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(
     const BiasArgs a, const BucketMap map, const int rows, const int64_t q_tiles,
     const int64_t k_tiles, const uint32_t per, float* __restrict__ part) {
@@ -484,21 +511,23 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_far_kernel(
   for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
   __syncthreads();
   const int64_t q0 = (qt * kGroups + group) * rows, k = kt * kKeys + x * V;
-  const int len = keys_left(k, a.K);
+  const int len = keys_left(k, a.K), rest = key_rest<T>(a.K);
   const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
   for (int s = 0; s < rows; s += kStep) {
     const int64_t q = q0 + s;
     typename Vec<T>::type raw[kStep];
 #pragma unroll
     for (int j = 0; j < kStep; ++j)
-      raw[j] = load_vec(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0);
+      raw[j] = load_vec<E>(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0, rest);
     float diag[kDiagonals];  // of difference k - q - 7 + i
 #pragma unroll
     for (int i = 0; i < kDiagonals; ++i) diag[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < kStep; ++j)
+    for (int j = 0; j < kStep; ++j) {
+      raw[j] = settle<E>(raw[j], q + j < a.Q ? len : 0, rest);
 #pragma unroll
       for (int u = 0; u < V; ++u) diag[kStep - 1 + u - j] += widen(raw[j][u]);
+    }
     // groups have windows of their own: no turns
     add_diagonals<V, kDiagonals, 1>(windows[group] + x * V + rows - kStep - s, diag, true, 0);
   }
@@ -575,56 +604,69 @@ size_t bias_grad_workspace_bytes(bool bf16, const BiasArgs& a, const BucketMap& 
   return static_cast<size_t>(a.H * map.num * grad_parts(bf16, a, map)) * sizeof(float);
 }
 
-template <typename T, int TX>
-static void launch_near(const BiasArgs& a, const BucketMap& map, const NearShape& s, float* part,
-                        hipStream_t stream) {
+// f(how rows of K keys end): gradients are only read, so that a row of a vector or
+// more may always be read with the elements before its end.
+template <typename T, typename F>
+static hipError_t by_key_end(int64_t K, F f) {
+  if (K % kVec<T> == 0) return f(std::integral_constant<End, End::kWhole>{});
+  return K > kVec<T> ? f(std::integral_constant<End, End::kOverlap>{})
+                     : f(std::integral_constant<End, End::kPieces>{});
+}
+template <typename T>
+static hipError_t launch_near(const BiasArgs& a, const BucketMap& map, const NearShape& s,
+                              float* part, hipStream_t stream) {
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(s.blocks, static_cast<uint32_t>(a.H)), dim3(kBiasThreads),
                        kBiasWaves * s.window * sizeof(float), stream, a, map,
                        static_cast<uint32_t>(s.q_steps), static_cast<uint32_t>(s.k_steps), s.units,
                        s.window, part);
+    return hipGetLastError();
   };
-  switch (s.qu) {
-    case 1: return launch(bias_grad_near_kernel<T, TX, 1>);
-    case 2: return launch(bias_grad_near_kernel<T, TX, 2>);
-    case 4: return launch(bias_grad_near_kernel<T, TX, 4>);
-    default: return launch(bias_grad_near_kernel<T, TX, 8>);
-  }
+  return by_key_end<T>(a.K, [&](auto end) {
+    return with_lanes<8, 16, 32, 64>(s.tx, [&](auto lanes) {
+      constexpr End E = end.value;
+      if constexpr (E == End::kPieces && lanes.value != 8) {
+        return hipErrorInvalidValue;  // not reached: less than a vector of keys has 8 lanes
+      } else {
+        return with_lanes<1, 2, 4, 8>(s.qu, [&](auto qu) {
+          return launch(bias_grad_near_kernel<T, lanes.value, qu.value, E>);
+        });
+      }
+    });
+  });
 }
 template <typename T>
-static void launch_far(const BiasArgs& a, const BucketMap& map, const FarShape& s, float* part,
-                       hipStream_t stream) {
+static hipError_t launch_far(const BiasArgs& a, const BucketMap& map, const FarShape& s, float* part,
+                             hipStream_t stream) {
   const TileGrid tg = tile_grid(a.B * a.H * s.q_tiles * s.k_tiles, 1);  // (bias_grad_fits)
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, tg.grid, dim3(kBiasThreads), 0, stream, a, map, s.rows, s.q_tiles,
                        s.k_tiles, tg.per, part);
+    return hipGetLastError();
   };
-  switch (s.tx) {
-    case 16: return launch(bias_grad_far_kernel<T, 16>);
-    case 32: return launch(bias_grad_far_kernel<T, 32>);
-    default: return launch(bias_grad_far_kernel<T, 64>);
-  }
+  return by_key_end<T>(a.K, [&](auto end) {
+    return with_lanes<16, 32, 64>(s.tx, [&](auto lanes) {
+      constexpr End E = end.value;
+      if constexpr (E == End::kPieces && lanes.value != 16) {
+        return hipErrorInvalidValue;  // not reached: less than a vector of keys has 16 lanes
+      } else {
+        return launch(bias_grad_far_kernel<T, lanes.value, E>);
+      }
+    });
+  });
 }
 template <typename T>
-static void launch_grad_t(const BiasArgs& a, const BucketMap& map, float* part, hipStream_t stream) {
-  if (!is_near(map)) return launch_far<T>(a, map, far_shape(sizeof(T) == 2, a), part, stream);
-  const NearShape s = near_shape(sizeof(T) == 2, a, map);
-  switch (s.tx) {
-    case 8: return launch_near<T, 8>(a, map, s, part, stream);
-    case 16: return launch_near<T, 16>(a, map, s, part, stream);
-    case 32: return launch_near<T, 32>(a, map, s, part, stream);
-    default: return launch_near<T, 64>(a, map, s, part, stream);
-  }
+static hipError_t launch_grad_t(const BiasArgs& a, const BucketMap& map, float* part,
+                                hipStream_t stream) {
+  return is_near(map) ? launch_near<T>(a, map, near_shape(sizeof(T) == 2, a, map), part, stream)
+                      : launch_far<T>(a, map, far_shape(sizeof(T) == 2, a), part, stream);
 }
 
 hipError_t launch_bias_grad(bool bf16, const BiasArgs& a, const BucketMap& map, void* workspace,
                             float* grad_table, hipStream_t stream) {
   float* part = static_cast<float*>(workspace);
-  if (bf16)
-    launch_grad_t<uint16_t>(a, map, part, stream);
-  else
-    launch_grad_t<float>(a, map, part, stream);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = bf16 ? launch_grad_t<uint16_t>(a, map, part, stream)
+                            : launch_grad_t<float>(a, map, part, stream);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(bias_sum_kernel, dim3(static_cast<uint32_t>(a.H * map.num)), dim3(kBiasThreads), 0,
                      stream, part, grad_parts(bf16, a, map), map.num, a.H, grad_table);

@@ -1,5 +1,7 @@
 // Operators on rows: dropout from a counter-based generator, layer norm and
 // its backward pass.
+#include <type_traits>
+
 #include "pss_rows.hpp"
 
 namespace pss {
@@ -14,6 +16,14 @@ __device__ __forceinline__ int cols_left(int64_t c, int64_t cols) {
   return cols - c > INT32_MAX ? INT32_MAX : static_cast<int>(cols - c);
 }
 
+// Which of the block's groups of G lanes: one value a wavefront for G = 64, so that
+// a row's addresses stay out of the lanes' registers.
+template <int G>
+__device__ __forceinline__ int group_of() {
+  const int g = threadIdx.x / G;
+  return G == kWave ? __builtin_amdgcn_readfirstlane(g) : g;
+}
+
 // Lanes to a row: as many as its pieces of 8, up to a wavefront.
 static int row_lanes(int64_t cols) {
   const int64_t pieces = (cols + kLanePiece - 1) / kLanePiece;
@@ -22,21 +32,30 @@ static int row_lanes(int64_t cols) {
   return g;
 }
 
+// f(a T, whether rows of `cols` end inside a vector)
+template <typename F>
+static hipError_t by_row_type(bool bf16, int64_t cols, F f) {
+  const std::true_type yes;
+  const std::false_type no;
+  if (bf16) return cols % kVec<uint16_t> ? f(uint16_t{}, yes) : f(uint16_t{}, no);
+  return cols % kVec<float> ? f(float{}, yes) : f(float{}, no);
+}
+
 // ---------------------------------------------------------------------------
 // out = residual + D(x): a span of a row to a group of G lanes.
 // ---------------------------------------------------------------------------
-template <typename T, int G>
+template <typename T, int G, bool ENDS>
 __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, const RowsIn residual,
                                                               const RowsOut out, const int64_t rows,
                                                               const int64_t cols,
                                                               const uint32_t spans,
                                                               const uint32_t per, const Drop drop,
                                                               const bool stream) {
-  typedef Span<T, G> S;
+  typedef Span<T, G, ENDS> S;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const uint32_t tile = tile_of(per, spans), span = blockIdx.x % spans;
   const int lane = threadIdx.x % G;
-  const int64_t r = static_cast<int64_t>(tile) * (kRowThreads / G) + threadIdx.x / G;
+  const int64_t r = static_cast<int64_t>(tile) * (kRowThreads / G) + group_of<G>();
   const int64_t c = static_cast<int64_t>(span) * (G * kLanePiece);
   if (r >= rows) return;
   const int left = cols_left(c, cols);
@@ -45,10 +64,12 @@ __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, co
   if (residual.p != nullptr)
     b.load(static_cast<const T*>(residual.p) + r * residual.stride + c, lane, left);
   float v[kLanePiece];
+  a.settle_end(lane, left);
   a.widen_to(v);
   if (drop.t) S::drop(v, drop, n, span * G, static_cast<uint32_t>(r), lane);
   if (residual.p != nullptr) {
     float q[kLanePiece];
+    b.settle_end(lane, left);
     b.widen_to(q);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) v[u] += q[u];
@@ -62,7 +83,7 @@ static bool streams(bool bf16, int64_t rows, int64_t cols) {
   return rows * cols * (bf16 ? 2 : 4) > kStreamBytes;
 }
 
-template <typename T>
+template <typename T, bool ENDS>
 static hipError_t launch_dropout_t(const RowsIn& x, const RowsIn& residual, const RowsOut& out,
                                    int64_t rows, int64_t cols, const Drop& drop,
                                    hipStream_t stream) {
@@ -78,20 +99,21 @@ static hipError_t launch_dropout_t(const RowsIn& x, const RowsIn& residual, cons
     return hipGetLastError();
   };
   switch (g) {
-    case 1: return launch(dropout_kernel<T, 1>);
-    case 2: return launch(dropout_kernel<T, 2>);
-    case 4: return launch(dropout_kernel<T, 4>);
-    case 8: return launch(dropout_kernel<T, 8>);
-    case 16: return launch(dropout_kernel<T, 16>);
-    case 32: return launch(dropout_kernel<T, 32>);
-    default: return launch(dropout_kernel<T, 64>);
+    case 1: return launch(dropout_kernel<T, 1, ENDS>);
+    case 2: return launch(dropout_kernel<T, 2, ENDS>);
+    case 4: return launch(dropout_kernel<T, 4, ENDS>);
+    case 8: return launch(dropout_kernel<T, 8, ENDS>);
+    case 16: return launch(dropout_kernel<T, 16, ENDS>);
+    case 32: return launch(dropout_kernel<T, 32, ENDS>);
+    default: return launch(dropout_kernel<T, 64, ENDS>);
   }
 }
 
 hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, const RowsOut& out,
                           int64_t rows, int64_t cols, const Drop& drop, hipStream_t stream) {
-  return bf16 ? launch_dropout_t<uint16_t>(x, residual, out, rows, cols, drop, stream)
-              : launch_dropout_t<float>(x, residual, out, rows, cols, drop, stream);
+  return by_row_type(bf16, cols, [&](auto t, auto ends) {
+    return launch_dropout_t<decltype(t), ends.value>(x, residual, out, rows, cols, drop, stream);
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -103,23 +125,26 @@ hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, co
 // ---------------------------------------------------------------------------
 
 // What a row needs of one span.
-template <typename T, int G>
+template <typename T, int G, bool ENDS>
 struct NormSpan {
-  Span<T, G> x, q;
-  __device__ __forceinline__ void load(const NormArgs& a, int64_t r, int64_t c, int lane, int left) {
-    x.load(static_cast<const T*>(a.x.p) + r * a.x.stride + c, lane, left);
+  Span<T, G, ENDS> x, q;
+  __device__ __forceinline__ void load(const NormArgs& a, int64_t r, int64_t c, int lane, int left,
+                                       bool there = true) {
+    x.load(static_cast<const T*>(a.x.p) + r * a.x.stride + c, lane, left, there);
     if (a.residual.p != nullptr)
-      q.load(static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, lane, left);
+      q.load(static_cast<const T*>(a.residual.p) + r * a.residual.stride + c, lane, left, there);
   }
   // s = residual + D(x)
   __device__ __forceinline__ void sum_to(float v[kLanePiece], const NormArgs& a, const Drop& drop,
-                                         uint64_t n, int64_t r, int64_t c, int lane) const {
+                                         uint64_t n, int64_t r, int64_t c, int lane, int left) {
+    x.settle_end(lane, left);
     x.widen_to(v);
     if (drop.t)
-      Span<T, G>::drop(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r),
-                       lane);
+      Span<T, G, ENDS>::drop(v, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r),
+                             lane);
     if (a.residual.p != nullptr) {
       float w[kLanePiece];
+      q.settle_end(lane, left);
       q.widen_to(w);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) v[u] += w[u];
@@ -127,11 +152,11 @@ struct NormSpan {
   }
 };
 
-template <typename T, int G>
+template <typename T, int G, bool ENDS>
 __device__ __forceinline__ void norm_store(float v[kLanePiece], const NormArgs& a, int64_t r,
                                            int64_t c, int lane, int left, float mean, float rstd,
                                            const float w[kLanePiece], const float b[kLanePiece]) {
-  typedef Span<T, G> S;
+  typedef Span<T, G, ENDS> S;
   if (a.sum.p != nullptr)
     S::store(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v, lane, left, a.stream);
 #pragma unroll
@@ -146,12 +171,13 @@ __device__ __forceinline__ void norm_store_stats(const NormArgs& a, int64_t r, f
 }
 
 // Squares of a span's elements about `mean`.
-template <typename T, int G>
+template <typename T, int G, bool ENDS>
 __device__ __forceinline__ float squares(const float v[kLanePiece], int lane, int left, float mean) {
   float sq = 0.f;
 #pragma unroll
   for (int u = 0; u < kLanePiece; ++u) {
-    const float e = Span<T, G>::col(lane, u) < left ? v[u] - mean : 0.f;
+    const int at = ENDS ? u : u / kVec<T> * kVec<T>;  // whole vectors are in or out
+    const float e = Span<T, G, ENDS>::col(lane, at) < left ? v[u] - mean : 0.f;
     sq += e * e;
   }
   return sq;
@@ -159,7 +185,7 @@ __device__ __forceinline__ float squares(const float v[kLanePiece], int lane, in
 
 // A group of G lanes a row, NP spans.  AHEAD: the next row is requested before the
 // present one's sums.  (4 wavefronts to a SIMD: at most 128 registers.)
-template <typename T, int G, int NP, bool AHEAD>
+template <typename T, int G, bool ENDS, int NP, bool AHEAD>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_group_kernel(const NormArgs a, const Drop drop) {
   constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
   const int lane = threadIdx.x % G;
@@ -167,44 +193,44 @@ __global__ __launch_bounds__(kRowThreads, 4) void norm_group_kernel(const NormAr
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
   const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
-  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / G;
-  NormSpan<T, G> in[NP], next[NP];
+  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + group_of<G>();
+  NormSpan<T, G, ENDS> in[NP], next[NP];
   float w[NP][kLanePiece], b[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    in[i].load(a, r, i * kSpan, lane, r < a.rows ? cols - i * kSpan : 0);
-    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
-    Span<T, G>::weights(b[i], a.bias, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 0.f);
+    in[i].load(a, r, i * kSpan, lane, cols - i * kSpan, r < a.rows);
+    Span<T, G, ENDS>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
+    Span<T, G, ENDS>::weights(b[i], a.bias, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 0.f);
   }
   for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows; r0 += step, r += step) {
     if (AHEAD && r0 + step < a.rows) {
 #pragma unroll
       for (int i = 0; i < NP; ++i)
-        next[i].load(a, r + step, i * kSpan, lane, r + step < a.rows ? cols - i * kSpan : 0);
+        next[i].load(a, r + step, i * kSpan, lane, cols - i * kSpan, r + step < a.rows);
     }
     float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      in[i].sum_to(v[i], a, drop, n, r, i * kSpan, lane);
+      in[i].sum_to(v[i], a, drop, n, r, i * kSpan, lane, cols - i * kSpan);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
     }
     const float mean = group_sum<G>(sum) * inv;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) sq += squares<T, G>(v[i], lane, cols - i * kSpan, mean);
+    for (int i = 0; i < NP; ++i) sq += squares<T, G, ENDS>(v[i], lane, cols - i * kSpan, mean);
     const float rstd = 1.f / sqrtf(group_sum<G>(sq) * inv + a.eps);
     if (r < a.rows) {
       if (lane == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
       for (int i = 0; i < NP; ++i)
-        norm_store<T, G>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
+        norm_store<T, G, ENDS>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       if (AHEAD)
         in[i] = next[i];
       else
-        in[i].load(a, r + step, i * kSpan, lane, r + step < a.rows ? cols - i * kSpan : 0);
+        in[i].load(a, r + step, i * kSpan, lane, cols - i * kSpan, r + step < a.rows);
     }
   }
 }
@@ -226,24 +252,24 @@ __device__ __forceinline__ float part_size(int k, int n, int cols) {
 // parts are joined through LDS with one barrier a row (the squares about the
 // common mean are those about each part's plus the part's size times the square
 // of its mean's distance).
-template <typename T, int TH, int NP, bool AHEAD>
+template <typename T, int TH, bool ENDS, int NP, bool AHEAD>
 __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2][2][kMaxWaves];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & (kWave - 1), wave = group_of<kWave>();
   const int waves = blockDim.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
   int64_t r = blockIdx.x;
-  NormSpan<T, kWave> in[NP], next[NP];
+  NormSpan<T, kWave, ENDS> in[NP], next[NP];
   float w[NP][kLanePiece], b[NP][kLanePiece];
   int c[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     c[i] = (i * waves + wave) * kSpanCols;
     in[i].load(a, r, c[i], lane, cols - c[i]);
-    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
-    Span<T, kWave>::weights(b[i], a.bias, a.weight_bf16, c[i], lane, cols - c[i], 0.f);
+    Span<T, kWave, ENDS>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
+    Span<T, kWave, ENDS>::weights(b[i], a.bias, a.weight_bf16, c[i], lane, cols - c[i], 0.f);
   }
   const float my_size = part_size<NP>(wave, waves, cols);
   const float inv_part = my_size > 0.f ? 1.f / my_size : 0.f;
@@ -259,13 +285,13 @@ __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, con
     float v[NP][kLanePiece], sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      in[i].sum_to(v[i], a, drop, n, r, c[i], lane);
+      in[i].sum_to(v[i], a, drop, n, r, c[i], lane, cols - c[i]);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) sum += v[i][u];
     }
     const float part = wave_sum(sum) * inv_part;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) sq += squares<T, kWave>(v[i], lane, cols - c[i], part);
+    for (int i = 0; i < NP; ++i) sq += squares<T, kWave, ENDS>(v[i], lane, cols - c[i], part);
     sq = wave_sum(sq);
     if (lane == 0) {
       lds[turn][0][wave] = part;
@@ -281,7 +307,7 @@ __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, con
     if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      norm_store<T, kWave>(v[i], a, r, c[i], lane, cols - c[i], mean, rstd, w[i], b[i]);
+      norm_store<T, kWave, ENDS>(v[i], a, r, c[i], lane, cols - c[i], mean, rstd, w[i], b[i]);
       if (AHEAD)
         in[i] = next[i];
       else if (after < a.rows)
@@ -312,21 +338,21 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
 // Wider rows: a block a row, which it reads three times (sum, squares about the
 // mean, result), the last two from L2.  Nothing is stored before the last pass,
 // where every element is read by the lane that then stores its results.
-template <typename T>
+template <typename T, bool ENDS>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2 * kRowWaves];
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t first = (threadIdx.x >> 6) * kSpanCols, step = kRowWaves * kSpanCols;
+  const int64_t first = group_of<kWave>() * kSpanCols, step = kRowWaves * kSpanCols;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const float inv = 1.f / static_cast<float>(a.cols);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     float sum = 0.f, zero = 0.f;
 #pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
-      NormSpan<T, kWave> in;
+      NormSpan<T, kWave, ENDS> in;
       float v[kLanePiece];
       in.load(a, r, c, lane, cols_left(c, a.cols));
-      in.sum_to(v, a, drop, n, r, c, lane);
+      in.sum_to(v, a, drop, n, r, c, lane, cols_left(c, a.cols));
       float piece = 0.f;  // of its own: a long row's chain of additions is 8 times shorter
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) piece += v[u];
@@ -337,25 +363,25 @@ __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArg
     float sq = 0.f;
 #pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
-      NormSpan<T, kWave> in;
+      NormSpan<T, kWave, ENDS> in;
       float v[kLanePiece];
       in.load(a, r, c, lane, cols_left(c, a.cols));
-      in.sum_to(v, a, drop, n, r, c, lane);
-      sq += squares<T, kWave>(v, lane, cols_left(c, a.cols), mean);
+      in.sum_to(v, a, drop, n, r, c, lane, cols_left(c, a.cols));
+      sq += squares<T, kWave, ENDS>(v, lane, cols_left(c, a.cols), mean);
     }
     block_sum2(sq, zero, lds);
     const float rstd = 1.f / sqrtf(sq * inv + a.eps);
     if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll 1
     for (int64_t c = first; c < a.cols; c += step) {
-      NormSpan<T, kWave> in;
+      NormSpan<T, kWave, ENDS> in;
       float v[kLanePiece], w[kLanePiece], b[kLanePiece];
       const int left = cols_left(c, a.cols);
       in.load(a, r, c, lane, left);
-      in.sum_to(v, a, drop, n, r, c, lane);
-      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
-      Span<T, kWave>::weights(b, a.bias, a.weight_bf16, c, lane, left, 0.f);
-      norm_store<T, kWave>(v, a, r, c, lane, left, mean, rstd, w, b);
+      in.sum_to(v, a, drop, n, r, c, lane, left);
+      Span<T, kWave, ENDS>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      Span<T, kWave, ENDS>::weights(b, a.bias, a.weight_bf16, c, lane, left, 0.f);
+      norm_store<T, kWave, ENDS>(v, a, r, c, lane, left, mean, rstd, w, b);
     }
   }
 }
@@ -393,7 +419,7 @@ static uint32_t row_blocks(const RowForm& f, int64_t rows) {
   return static_cast<uint32_t>((want + rounds - 1) / rounds);
 }
 
-template <typename T>
+template <typename T, bool ENDS>
 static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t stream) {
   // 128 registers a lane at most: 16 wavefronts to a CU
   const RowForm f = row_form(a.cols, 16, 16, kMaxWaves);
@@ -404,28 +430,30 @@ static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop);
     return hipGetLastError();
   };
-  if (f.spans == 0) return launch(norm_wide_kernel<T>);
+  if (f.spans == 0) return launch(norm_wide_kernel<T, ENDS>);
   if (f.lanes > kWave) {
-    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, 1, true>);
-    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, 2, kAhead2>)
-                          : launch(norm_block_kernel<T, 1024, 2, false>);
+    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, ENDS, 1, true>);
+    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, ENDS, 2, kAhead2>)
+                          : launch(norm_block_kernel<T, 1024, ENDS, 2, false>);
   }
   switch (f.lanes * f.spans) {
-    case 1: return launch(norm_group_kernel<T, 1, 1, true>);
-    case 2: return launch(norm_group_kernel<T, 2, 1, true>);
-    case 4: return launch(norm_group_kernel<T, 4, 1, true>);
-    case 8: return launch(norm_group_kernel<T, 8, 1, true>);
-    case 16: return launch(norm_group_kernel<T, 16, 1, true>);
-    case 32: return launch(norm_group_kernel<T, 32, 1, true>);
-    case 64: return launch(norm_group_kernel<T, 64, 1, true>);
-    default: return launch(norm_group_kernel<T, 64, 2, kAhead2>);
+    case 1: return launch(norm_group_kernel<T, 1, ENDS, 1, true>);
+    case 2: return launch(norm_group_kernel<T, 2, ENDS, 1, true>);
+    case 4: return launch(norm_group_kernel<T, 4, ENDS, 1, true>);
+    case 8: return launch(norm_group_kernel<T, 8, ENDS, 1, true>);
+    case 16: return launch(norm_group_kernel<T, 16, ENDS, 1, true>);
+    case 32: return launch(norm_group_kernel<T, 32, ENDS, 1, true>);
+    case 64: return launch(norm_group_kernel<T, 64, ENDS, 1, true>);
+    default: return launch(norm_group_kernel<T, 64, ENDS, 2, kAhead2>);
   }
 }
 
 hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStream_t stream) {
   NormArgs a = args;
   a.stream = streams(bf16, a.rows, a.cols);
-  return bf16 ? launch_norm_t<uint16_t>(a, drop, stream) : launch_norm_t<float>(a, drop, stream);
+  return by_row_type(bf16, a.cols, [&](auto t, auto ends) {
+    return launch_norm_t<decltype(t), ends.value>(a, drop, stream);
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -436,21 +464,23 @@ hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStr
 // ---------------------------------------------------------------------------
 
 // What a row needs of one span.
-template <typename T, int G>
+template <typename T, int G, bool ENDS>
 struct GradSpan {
-  Span<T, G> dy, s, up;
+  Span<T, G, ENDS> dy, s, up;
   __device__ __forceinline__ void load(const NormGradArgs& a, int64_t r, int64_t c, int lane,
-                                       int left) {
-    dy.load(static_cast<const T*>(a.grad.p) + r * a.grad.stride + c, lane, left);
-    s.load(static_cast<const T*>(a.s.p) + r * a.s.stride + c, lane, left);
+                                       int left, bool there = true) {
+    dy.load(static_cast<const T*>(a.grad.p) + r * a.grad.stride + c, lane, left, there);
+    s.load(static_cast<const T*>(a.s.p) + r * a.s.stride + c, lane, left, there);
     if (a.grad_sum.p != nullptr)
-      up.load(static_cast<const T*>(a.grad_sum.p) + r * a.grad_sum.stride + c, lane, left);
+      up.load(static_cast<const T*>(a.grad_sum.p) + r * a.grad_sum.stride + c, lane, left, there);
   }
   // The row's two sums, and this span's part of the gradients over rows.
   __device__ __forceinline__ void sums(const float w[kLanePiece], float mean, float rstd, float& sh,
-                                       float& shz, float gw[kLanePiece],
-                                       float gb[kLanePiece]) const {
+                                       float& shz, float gw[kLanePiece], float gb[kLanePiece],
+                                       int lane, int left) {
     float d[kLanePiece], z[kLanePiece];
+    dy.settle_end(lane, left);
+    s.settle_end(lane, left);
     dy.widen_to(d);
     s.widen_to(z);
 #pragma unroll
@@ -469,7 +499,7 @@ struct GradSpan {
   __device__ __forceinline__ void finish(const float w[kLanePiece], float mean, float rstd, float m1,
                                          float m2, const NormGradArgs& a, const Drop& drop,
                                          uint64_t n, int64_t r, int64_t c, int lane, int left) {
-    typedef Span<T, G> S;
+    typedef Span<T, G, ENDS> S;
     float d[kLanePiece], z[kLanePiece];
     dy.renew();
     s.renew();
@@ -481,6 +511,7 @@ struct GradSpan {
       d[u] = rstd * (d[u] * w[u] - m1 - z[u] * m2);
     }
     if (a.grad_sum.p != nullptr) {
+      up.settle_end(lane, left);
       up.widen_to(z);
 #pragma unroll
       for (int u = 0; u < kLanePiece; ++u) d[u] += z[u];
@@ -498,8 +529,8 @@ struct GradSpan {
 
 // A group of G lanes a row, as in norm_group_kernel; a lane keeps its columns'
 // weights and gradient sums for all of its rows.
-template <typename T, int G, int NP>
-__global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const NormGradArgs a,
+template <typename T, int G, bool ENDS, int NP>
+__global__ __launch_bounds__(kRowThreads, NP == 1 ? 4 : 2) void norm_grad_group_kernel(const NormGradArgs a,
                                                                       const Drop drop,
                                                                       float* part) {
   constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
@@ -509,13 +540,13 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
   const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
-  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / G;
-  GradSpan<T, G> in[NP], next[NP];
+  int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + group_of<G>();
+  GradSpan<T, G, ENDS> in[NP], next[NP];
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    in[i].load(a, r, i * kSpan, lane, r < a.rows ? cols - i * kSpan : 0);
-    Span<T, G>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
+    in[i].load(a, r, i * kSpan, lane, cols - i * kSpan, r < a.rows);
+    Span<T, G, ENDS>::weights(w[i], a.weight, a.weight_bf16, i * kSpan, lane, cols - i * kSpan, 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
@@ -526,7 +557,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
       const bool more = r + step < a.rows;
 #pragma unroll
       for (int i = 0; i < NP; ++i)
-        next[i].load(a, r + step, i * kSpan, lane, more ? cols - i * kSpan : 0);
+        next[i].load(a, r + step, i * kSpan, lane, cols - i * kSpan, more);
       if (more) {
         next_mean = a.mean[r + step];
         next_rstd = a.rstd[r + step];
@@ -534,7 +565,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
     }
     float sh = 0.f, shz = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i]);
+    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i], lane, cols - i * kSpan);
     const float m1 = group_sum<G>(sh) * inv, m2 = group_sum<G>(shz) * inv;
     if (r < a.rows) {
 #pragma unroll
@@ -558,7 +589,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
         float v = which ? gb[i][u] : gw[i][u];
 #pragma unroll
         for (int m = G; m < kWave; m <<= 1) v += __shfl_xor(v, m);
-        if ((threadIdx.x & (kWave - 1)) < G) lds[wave][i * kSpan + Span<T, G>::col(lane, u)] = v;
+        if ((threadIdx.x & (kWave - 1)) < G) lds[wave][i * kSpan + Span<T, G, ENDS>::col(lane, u)] = v;
       }
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += kRowThreads) {
@@ -572,24 +603,24 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_group_kernel(const Norm
 
 // A block a row: its wavefronts' two sums are joined through LDS with one
 // barrier a row.
-template <typename T, int TH, int NP>
+template <typename T, int TH, bool ENDS, int NP>
 __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs a, const Drop drop,
                                                              float* part) {
   __shared__ float lds[2][2][kMaxWaves];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & (kWave - 1), wave = group_of<kWave>();
   const int waves = blockDim.x >> 6;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const int cols = static_cast<int>(a.cols);
   const float inv = 1.f / static_cast<float>(cols);
   int64_t r = blockIdx.x;
-  GradSpan<T, kWave> in[NP], next[NP];
+  GradSpan<T, kWave, ENDS> in[NP], next[NP];
   float w[NP][kLanePiece], gw[NP][kLanePiece], gb[NP][kLanePiece];
   int c[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     c[i] = (i * waves + wave) * kSpanCols;
     in[i].load(a, r, c[i], lane, cols - c[i]);
-    Span<T, kWave>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
+    Span<T, kWave, ENDS>::weights(w[i], a.weight, a.weight_bf16, c[i], lane, cols - c[i], 1.f);
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) gw[i][u] = gb[i][u] = 0.f;
   }
@@ -606,7 +637,7 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
     const float next_mean = more ? a.mean[after] : 0.f, next_rstd = more ? a.rstd[after] : 0.f;
     float sh = 0.f, shz = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i]);
+    for (int i = 0; i < NP; ++i) in[i].sums(w[i], mean, rstd, sh, shz, gw[i], gb[i], lane, cols - c[i]);
     sh = wave_sum(sh);
     shz = wave_sum(shz);
     if (lane == 0) {
@@ -628,29 +659,31 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
   float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    Span<T, kWave>::store(mine + c[i], gw[i], lane, cols - c[i], false);
-    Span<T, kWave>::store(mine + cols + c[i], gb[i], lane, cols - c[i], false);
+    Span<T, kWave, ENDS>::store(mine + c[i], gw[i], lane, cols - c[i], false);
+    Span<T, kWave, ENDS>::store(mine + cols + c[i], gb[i], lane, cols - c[i], false);
   }
 }
 
 // Wider rows.  First the rows' two means (m1 and m2, [2][rows] of scratch) ...
-template <typename T>
+template <typename T, bool ENDS>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_means_kernel(const NormGradArgs a,
                                                                       float* __restrict__ means) {
   __shared__ float lds[2 * kRowWaves];
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t begin = (threadIdx.x >> 6) * kSpanCols, step = kRowWaves * kSpanCols;
+  const int64_t begin = group_of<kWave>() * kSpanCols, step = kRowWaves * kSpanCols;
   const float inv = 1.f / static_cast<float>(a.cols);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sh = 0.f, shz = 0.f;
     for (int64_t c = begin; c < a.cols; c += step) {
       const int left = cols_left(c, a.cols);
-      Span<T, kWave> g, s;
+      Span<T, kWave, ENDS> g, s;
       float dy[kLanePiece], z[kLanePiece], w[kLanePiece];
       g.load(static_cast<const T*>(a.grad.p) + r * a.grad.stride + c, lane, left);
       s.load(static_cast<const T*>(a.s.p) + r * a.s.stride + c, lane, left);
-      Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      Span<T, kWave, ENDS>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+      g.settle_end(lane, left);
+      s.settle_end(lane, left);
       g.widen_to(dy);
       s.widen_to(z);
       float ph = 0.f, phz = 0.f;
@@ -672,30 +705,30 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_means_kernel(const Norm
 }
 // ... then tiles of columns, a wavefront a span of them: block y takes rows y, y +
 // gridDim.y, ... and keeps its columns' gradient sums in registers.
-template <typename T>
+template <typename T, bool ENDS>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_tile_kernel(
     const NormGradArgs a, const Drop drop, const float* __restrict__ means, float* part) {
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kRowWaves + (threadIdx.x >> 6)) * kSpanCols;
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * kRowWaves + group_of<kWave>()) * kSpanCols;
   if (c >= a.cols) return;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const int left = cols_left(c, a.cols);
   float w[kLanePiece], gw[kLanePiece], gb[kLanePiece];
-  Span<T, kWave>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
+  Span<T, kWave, ENDS>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
 #pragma unroll
   for (int u = 0; u < kLanePiece; ++u) gw[u] = gb[u] = 0.f;
   for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
-    GradSpan<T, kWave> in;
+    GradSpan<T, kWave, ENDS> in;
     in.load(a, r, c, lane, left);
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sh = 0.f, shz = 0.f;
-    in.sums(w, mean, rstd, sh, shz, gw, gb);
+    in.sums(w, mean, rstd, sh, shz, gw, gb, lane, left);
     in.finish(w, mean, rstd, means[r], means[a.rows + r], a, drop, n, r, c, lane, left);
   }
   if (part == nullptr) return;
   float* mine = part + static_cast<int64_t>(blockIdx.y) * 2 * a.cols + c;
-  Span<T, kWave>::store(mine, gw, lane, left, false);
-  Span<T, kWave>::store(mine + a.cols, gb, lane, left, false);
+  Span<T, kWave, ENDS>::store(mine, gw, lane, left, false);
+  Span<T, kWave, ENDS>::store(mine + a.cols, gb, lane, left, false);
 }
 
 // Sums the blocks' parts: 16 columns a block, 64 threads to each, which request
@@ -761,36 +794,37 @@ size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols, bool sums) {
   return (part + (grad_form(cols).spans == 0 ? 2 * static_cast<size_t>(rows) : 0)) * sizeof(float);
 }
 
-template <typename T>
-static void launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, float* means,
+template <typename T, bool ENDS>
+static hipError_t launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, float* means,
                                int parts, hipStream_t stream) {
   const RowForm f = grad_form(a.cols);
   const dim3 grid(parts), block(f.lanes <= kWave ? kRowThreads : f.lanes);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop, part);
+    return hipGetLastError();
   };
   if (f.spans == 0) {
     const int64_t most = 2048;
-    hipLaunchKernelGGL(norm_grad_means_kernel<T>,
+    hipLaunchKernelGGL((norm_grad_means_kernel<T, ENDS>),
                        dim3(static_cast<uint32_t>(a.rows < most ? a.rows : most)), block, 0, stream,
                        a, means);
     const int64_t tiles = (a.cols + kRowWaves * kSpanCols - 1) / (kRowWaves * kSpanCols);
-    hipLaunchKernelGGL(norm_grad_tile_kernel<T>, dim3(static_cast<uint32_t>(tiles), parts), block, 0,
+    hipLaunchKernelGGL((norm_grad_tile_kernel<T, ENDS>), dim3(static_cast<uint32_t>(tiles), parts), block, 0,
                        stream, a, drop, means, part);
-    return;
+    return hipGetLastError();
   }
   if (f.lanes > kWave)
-    return f.spans == 1 ? launch(norm_grad_block_kernel<T, 1024, 1>)
-                        : launch(norm_grad_block_kernel<T, 512, 2>);
+    return f.spans == 1 ? launch(norm_grad_block_kernel<T, 1024, ENDS, 1>)
+                        : launch(norm_grad_block_kernel<T, 512, ENDS, 2>);
   switch (f.lanes * f.spans) {
-    case 1: return launch(norm_grad_group_kernel<T, 1, 1>);
-    case 2: return launch(norm_grad_group_kernel<T, 2, 1>);
-    case 4: return launch(norm_grad_group_kernel<T, 4, 1>);
-    case 8: return launch(norm_grad_group_kernel<T, 8, 1>);
-    case 16: return launch(norm_grad_group_kernel<T, 16, 1>);
-    case 32: return launch(norm_grad_group_kernel<T, 32, 1>);
-    case 64: return launch(norm_grad_group_kernel<T, 64, 1>);
-    default: return launch(norm_grad_group_kernel<T, 64, 2>);
+    case 1: return launch(norm_grad_group_kernel<T, 1, ENDS, 1>);
+    case 2: return launch(norm_grad_group_kernel<T, 2, ENDS, 1>);
+    case 4: return launch(norm_grad_group_kernel<T, 4, ENDS, 1>);
+    case 8: return launch(norm_grad_group_kernel<T, 8, ENDS, 1>);
+    case 16: return launch(norm_grad_group_kernel<T, 16, ENDS, 1>);
+    case 32: return launch(norm_grad_group_kernel<T, 32, ENDS, 1>);
+    case 64: return launch(norm_grad_group_kernel<T, 64, ENDS, 1>);
+    default: return launch(norm_grad_group_kernel<T, 64, ENDS, 2>);
   }
 }
 
@@ -802,11 +836,9 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& dro
   const int parts = norm_grad_parts(a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;
   float* means = static_cast<float*>(workspace) + (sums ? static_cast<size_t>(parts) * 2 * a.cols : 0);
-  if (bf16)
-    launch_norm_grad_t<uint16_t>(a, drop, part, means, parts, stream);
-  else
-    launch_norm_grad_t<float>(a, drop, part, means, parts, stream);
-  hipError_t e = hipGetLastError();
+  hipError_t e = by_row_type(bf16, a.cols, [&](auto t, auto ends) {
+    return launch_norm_grad_t<decltype(t), ends.value>(a, drop, part, means, parts, stream);
+  });
   if (e == hipSuccess && sums) {
     const int64_t blocks = (2 * a.cols + kSumCols - 1) / kSumCols;
     hipLaunchKernelGGL(sum_parts_kernel,

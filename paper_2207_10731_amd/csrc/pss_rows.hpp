@@ -129,7 +129,10 @@ __device__ __forceinline__ uint64_t drop_offset(const Drop& d) {
 
 // Vectors in memory: 16-byte loads and stores at any element (the memory system
 // takes them at any alignment of whole elements).
+typedef float f2_any __attribute__((ext_vector_type(2), aligned(4)));
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t w1_any __attribute__((aligned(2)));
+typedef uint32_t w2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint16_t h4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint16_t h8_any __attribute__((ext_vector_type(8), aligned(2)));
 template <typename T>
@@ -148,16 +151,98 @@ constexpr int kVec = 16 / static_cast<int>(sizeof(T));
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(uint16_t x) { return bf16_to_f32(x); }
 
+// The end of a row whose length is not a whole number of vectors: n of its last
+// vector's elements, n = rest (the same in every lane).  kOverlap: one load that
+// also takes elements before them, moved down when the vector is used (settle), by
+// which time it has arrived; for rows of at least a vector that one wavefront
+// alone reads and writes (a result stored in place by another one may be there).
+// kPieces: loads of 8, 4 and 2 bytes.  Rows of whole vectors need neither, and
+// kernels of their own save the registers (norm of 32768 x 1024 bfloat16: 28 us,
+// with the code for ends 33).
+enum class End { kWhole, kOverlap, kPieces };
+
+__device__ __forceinline__ f4_any load_end(const float* p, int rest) {
+  f4_any x = {0.f, 0.f, 0.f, 0.f};
+  if (rest & 2) {
+    const f2_any a = __builtin_nontemporal_load(reinterpret_cast<const f2_any*>(p));
+    x[0] = a[0];
+    x[1] = a[1];
+  }
+  if (rest & 1) x[2] = __builtin_nontemporal_load(p + (rest & 2));
+  return x;
+}
+__device__ __forceinline__ h8_any load_end(const uint16_t* p, int rest) {
+  uint32_t w[4] = {0, 0, 0, 0};
+  if (rest & 4) {
+    const w2_any a = __builtin_nontemporal_load(reinterpret_cast<const w2_any*>(p));
+    w[0] = a[0];
+    w[1] = a[1];
+  }
+  if (rest & 2) w[2] = __builtin_nontemporal_load(reinterpret_cast<const w1_any*>(p + (rest & 4)));
+  if (rest & 1) w[3] = __builtin_nontemporal_load(p + (rest & 6));
+  h8_any x;
+  __builtin_memcpy(&x, w, 16);
+  return x;
+}
+
 // Rows are read once: past the caches (their lines are not kept for others),
 // which for a large copy of float32 is 6.2 against 5.8 TB/s.  n elements from p
-// on (kVec or more: all); the others are 0.
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::type load_vec(const T* p, int n) {
+// on (kVec or more: all, 0 or less: none); the others are 0 once it is settled.
+template <End E, typename T>
+__device__ __forceinline__ typename Vec<T>::type load_vec(const T* p, int n, int rest) {
   typedef typename Vec<T>::type V;
-  if (n >= kVec<T>) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
-  V x;
+  if (E == End::kWhole ? n > 0 : n >= kVec<T>)
+    return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  V x = 0;
+  if (E == End::kOverlap && n > 0)
+    x = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + rest - kVec<T>));
+  if (E == End::kPieces && n > 0) x = load_end(p, rest);
+  return x;
+}
+
+template <End E>
+__device__ __forceinline__ f4_any settle(f4_any x, int n, int rest) {
+  if (E == End::kWhole || n <= 0 || n >= 4) return x;
+  if (E == End::kOverlap) {
+    const int by = 4 - rest;
+    if (by & 1) x = f4_any{x[1], x[2], x[3], 0.f};
+    if (by & 2) x = f4_any{x[2], x[3], 0.f, 0.f};
+  } else if (!(rest & 2)) {
+    x = f4_any{x[2], 0.f, 0.f, 0.f};
+  }
+  return x;
+}
+template <End E>
+__device__ __forceinline__ h8_any settle(h8_any x, int n, int rest) {
+  if (E == End::kWhole || n <= 0 || n >= 8) return x;
+  uint32_t w[4];
+  __builtin_memcpy(w, &x, 16);
+  if (E == End::kOverlap) {
+    const int by = 8 - rest;
+    if (by & 1) {
 #pragma unroll
-  for (int u = 0; u < kVec<T>; ++u) x[u] = u < n ? p[u] : T{0};
+      for (int i = 0; i < 4; ++i) w[i] = w[i] >> 16 | (i < 3 ? w[i + 1] << 16 : 0);
+    }
+    if (by & 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = i < 3 ? w[i + 1] : 0;
+    }
+    if (by & 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = i < 2 ? w[i + 2] : 0;
+    }
+  } else {
+    if (!(rest & 2)) {
+      w[2] = w[3];
+      w[3] = 0;
+    }
+    if (!(rest & 4)) {
+      w[0] = w[2];
+      w[1] = w[3];
+      w[2] = w[3] = 0;
+    }
+  }
+  __builtin_memcpy(&x, w, 16);
   return x;
 }
 
@@ -183,20 +268,40 @@ __device__ __forceinline__ h8_any narrow(const float* v, uint16_t) {
   }
   return a;
 }
-// stream: past the caches (results too large for them).
-template <typename T>
+// Stores of a row's end by halves of the vector.
+__device__ __forceinline__ void store_end(float* p, f4_any a, int n) {
+  if (n & 2) *reinterpret_cast<f2_any*>(p) = f2_any{a[0], a[1]};
+  if (n & 1) p[n & 2] = n & 2 ? a[2] : a[0];
+}
+__device__ __forceinline__ void store_end(uint16_t* p, h8_any a, int n) {
+  uint32_t w[4];
+  __builtin_memcpy(w, &a, 16);
+  if (n & 4) {
+    *reinterpret_cast<w2_any*>(p) = w2_any{w[0], w[1]};
+    p += 4;
+    w[0] = w[2];
+    w[1] = w[3];
+  }
+  if (n & 2) {
+    *reinterpret_cast<w1_any*>(p) = w[0];
+    p += 2;
+    w[0] = w[1];
+  }
+  if (n & 1) *p = static_cast<uint16_t>(w[0]);
+}
+// stream: past the caches (results too large for them); ENDS: n may be below kVec
+// and above 0.
+template <bool ENDS, typename T>
 __device__ __forceinline__ void store_vec(T* p, const float* v, int n, bool stream) {
   typedef typename Vec<T>::type V;
   const V a = narrow(v, T{});
-  if (n >= kVec<T>) {
+  if (ENDS ? n >= kVec<T> : n > 0) {
     if (stream)
       __builtin_nontemporal_store(a, reinterpret_cast<V*>(p));
     else
       *reinterpret_cast<V*>(p) = a;
-  } else {
-#pragma unroll
-    for (int u = 0; u < kVec<T>; ++u)
-      if (u < n) p[u] = a[u];
+  } else if (ENDS && n > 0) {
+    store_end(p, a, n);
   }
 }
 
@@ -205,21 +310,32 @@ __device__ __forceinline__ void store_vec(T* p, const float* v, int n, bool stre
 // 16 bytes apart: a bfloat16 lane has columns 8 lane .. 8 lane + 7, a float32 lane
 // 4 lane .. 4 lane + 3 and the same of the span's second half (32 bytes apart a
 // large float32 copy runs at 5.2 to 5.9 TB/s, 16 apart at 5.8 to 6.2).
-template <typename T, int G>
+// ENDS: rows may end inside a vector.
+template <typename T, int G, bool ENDS>
 struct Span {
+  static constexpr End kEnd = !ENDS ? End::kWhole : (G > 1 && G < kWave ? End::kOverlap : End::kPieces);
   static constexpr int kParts = kLanePiece / kVec<T>;
   typename Vec<T>::type q[kParts];
 
   static __device__ __forceinline__ int col(int lane, int u) {
     return u / kVec<T> * (G * kVec<T>) + lane * kVec<T> + u % kVec<T>;
   }
-  // p: the span's first column; left: columns from there to the row's end.
-  __device__ __forceinline__ void load(const T* p, int lane, int left) {
+  // Elements of the last vector of a row that ends `left` columns on.
+  static __device__ __forceinline__ int rest(int left) { return left & (kVec<T> - 1); }
+  // p: the span's first column; left: columns from there to the row's end; there:
+  // false for a row past the last.
+  __device__ __forceinline__ void load(const T* p, int lane, int left, bool there = true) {
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
       const int c = col(lane, i * kVec<T>);
-      q[i] = load_vec(p + c, left - c);
+      q[i] = load_vec<kEnd>(p + c, there ? left - c : 0, rest(left));
     }
+  }
+  // Before the span's elements are used.
+  __device__ __forceinline__ void settle_end(int lane, int left) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+      q[i] = settle<kEnd>(q[i], left - col(lane, i * kVec<T>), rest(left));
   }
   // From here on the compiler takes the span as new: values made from it before
   // are made again rather than kept in registers.
@@ -241,7 +357,7 @@ struct Span {
     constexpr int V = kVec<O> < kVec<T> ? kVec<O> : kVec<T>;  // consecutive columns
 #pragma unroll
     for (int u = 0; u < kLanePiece; u += V)
-      store_vec(p + col(lane, u), v + u, left - col(lane, u), stream);
+      store_vec<ENDS>(p + col(lane, u), v + u, left - col(lane, u), stream);
   }
   // Weights (bf16: their storage) from column c0 on in the span's layout; null:
   // `fill`.  Other blocks read them too: through the caches, in fours.
@@ -260,7 +376,7 @@ struct Span {
           const h4_any x = *reinterpret_cast<const h4_any*>(p);
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[u + k] = bf16_to_f32(x[k]);
-        } else {
+        } else if (ENDS) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             if (c + k < left) v[u + k] = bf16_to_f32(p[k]);
@@ -271,7 +387,7 @@ struct Span {
           const f4_any x = *reinterpret_cast<const f4_any*>(p);
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[u + k] = x[k];
-        } else {
+        } else if (ENDS) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             if (c + k < left) v[u + k] = p[k];

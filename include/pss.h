@@ -451,7 +451,8 @@ int pss_layer_norm_forward(const pss_rows_params* params, const pss_dropout_para
  * grad_x, grad_residual: row arguments; grad_weight, grad_bias: device
  * float32[C], overwritten.  Each may be NULL if it is not wanted (one at
  * least is not).  The sums over rows are taken in a fixed order that depends
- * on R and C alone: bit-identical from run to run. */
+ * on R, C and the type alone: bit-identical from run to run.  (The gradient of
+ * a row argument that every row shares, stride 0, is the sum of the rows'.) */
 int pss_layer_norm_backward(const pss_rows_params* params, const pss_dropout_params* dropout,
                             const void* grad_out, int64_t grad_out_stride, const void* s,
                             int64_t s_stride, const void* weight, const float* mean,

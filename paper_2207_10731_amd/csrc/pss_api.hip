@@ -1112,14 +1112,14 @@ int pss_layer_norm_backward(const pss_rows_params* params, const pss_dropout_par
   a.rows = params->rows;
   a.cols = params->cols;
   CallScratch scratch;
+  const bool bf16 = params->dtype == PSS_BF16;
   const size_t need = pss::norm_grad_workspace_bytes(
-      a.rows, a.cols, grad_weight != nullptr || grad_bias != nullptr);
+      bf16, a.rows, a.cols, grad_weight != nullptr || grad_bias != nullptr);
   if (need > 0) {
     st = scratch.take(need, stream);
     if (st != PSS_OK) return st;
   }
-  const hipError_t e =
-      pss::launch_norm_grad(params->dtype == PSS_BF16, a, drop, scratch.ptr(), stream);
+  const hipError_t e = pss::launch_norm_grad(bf16, a, drop, scratch.ptr(), stream);
   const hipError_t ef = scratch.done();
   return (e != hipSuccess || ef != hipSuccess) ? PSS_ERR_HIP : PSS_OK;
 } catch (...) {  // no host memory for the scratch's record

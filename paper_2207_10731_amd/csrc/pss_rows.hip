@@ -393,20 +393,28 @@ struct RowForm {
   int spans;  // of a lane; 0: the wide kernel
   int waves;  // of a CU
 };
-// waves1, waves2: those of the kernels with one and two spans a lane; most:
-// wavefronts of a block.
-static RowForm row_form(int64_t cols, int waves1, int waves2, int most) {
+constexpr int kHeld = 16;     // wavefronts of 128 registers
+constexpr int kHeldBf16 = 20;  // of the forward's bfloat16 kernel of one span
+
+// Blocks of whole wavefronts beyond 1024 columns, one or two spans a lane.  Two hold
+// more rows on a CU but need more registers: bfloat16 takes them for half as many
+// rows again (8192 x 4096: 28 against 34 us; 25000 x 1300, 8 rows against 6: 45
+// against 37), float32, whose spans are twice the bytes, only where a CU would be
+// left with one row (4096 x 8192: 49 against 55 us; 8192 x 4096 with residual, 4 rows
+// against 2: 100 against 94).  Two-span blocks of an odd number of wavefronts leave a
+// SIMD without its share (8192 x 4104 float32: 5 wavefronts 57 us, 6 54).
+static RowForm norm_form(bool bf16, int64_t cols) {
   const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
-  if (n <= kWave) return {row_lanes(cols), 1, waves1};
-  if (n <= 2 * kWave) return {kWave, 2, waves2};
-  // a block of whole wavefronts, one or two spans a lane: what keeps more
-  // spans on a CU
-  const int64_t w1 = (n + kWave - 1) / kWave, w2 = (n + 2 * kWave - 1) / (2 * kWave);
-  const int64_t held1 = w1 <= most ? waves1 / w1 * w1 : 0;
-  const int64_t held2 = w2 <= most ? 2 * (waves2 / w2 * w2) : 0;
-  if (held1 == 0 && held2 == 0) return {kRowThreads, 0, kRowWaves};
-  if (held1 >= held2) return {static_cast<int>(w1) * kWave, 1, waves1};
-  return {static_cast<int>(w2) * kWave, 2, waves2};
+  if (n <= kWave) return {row_lanes(cols), 1, kHeld};
+  if (n <= 2 * kWave) return {kWave, 2, kHeld};
+  const int64_t w1 = (n + kWave - 1) / kWave, half = (n + 2 * kWave - 1) / (2 * kWave);
+  const int64_t w2 = half > 1 ? (half + 1) / 2 * 2 : 1;
+  if (w2 > kMaxWaves) return {kRowThreads, 0, kRowWaves};
+  const int64_t held = bf16 ? kHeldBf16 : kHeld;
+  const int64_t rows1 = w1 <= kMaxWaves ? held / w1 : 0, rows2 = kHeld / w2;
+  const bool two = rows1 == 0 || (bf16 ? 2 * rows2 >= 3 * rows1 : rows1 == 1 && rows2 > 1);
+  if (two) return {static_cast<int>(w2) * kWave, 2, kHeld};
+  return {static_cast<int>(w1) * kWave, 1, static_cast<int>(held)};
 }
 // Blocks that walk rows: what the CUs hold, with as many rows to each (a second
 // round of blocks would take as long as the first).
@@ -421,8 +429,7 @@ static uint32_t row_blocks(const RowForm& f, int64_t rows) {
 
 template <typename T, bool ENDS>
 static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t stream) {
-  // 128 registers a lane at most: 16 wavefronts to a CU
-  const RowForm f = row_form(a.cols, 16, 16, kMaxWaves);
+  const RowForm f = norm_form(sizeof(T) == 2, a.cols);
   const dim3 grid(f.spans ? row_blocks(f, a.rows) : static_cast<uint32_t>(a.rows < 2048 ? a.rows : 2048));
   const dim3 block(f.lanes <= kWave ? kRowThreads : f.lanes);
   constexpr bool kAhead2 = sizeof(T) == 2;  // two float32 spans ahead: too many registers
@@ -776,28 +783,43 @@ __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* __r
   }
 }
 
-// One span a lane takes up to 128 registers, two up to 256.
-static RowForm grad_form(int64_t cols) { return row_form(cols, 16, 8, kMaxWaves); }
+// One span a lane takes up to 128 registers, two bfloat16 ones up to 170: blocks of
+// two are for rows that one span does not cover (4000 x 9000 bfloat16: 59 us, the
+// wide form 91; float32 they would spill, 217 against 208 with residual).  Five
+// wavefronts a block leave a SIMD without its share: 6 (16000 x 2500 bfloat16: 70
+// against 86 us).
+constexpr int kGradWaves2 = 12;
+static RowForm grad_form(bool bf16, int64_t cols) {
+  const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
+  if (n <= kWave) return {row_lanes(cols), 1, kHeld};
+  if (n <= 2 * kWave) return {kWave, 2, kHeld / 2};
+  const int64_t w = (n + kWave - 1) / kWave, w1 = w > 3 ? (w + 1) / 2 * 2 : w;
+  if (w1 <= kMaxWaves) return {static_cast<int>(w1) * kWave, 1, kHeld};
+  const int64_t w2 = (n + 2 * kWave - 1) / (2 * kWave);
+  if (bf16 && w2 <= kGradWaves2) return {static_cast<int>(w2) * kWave, 2, kGradWaves2};
+  return {kRowThreads, 0, kRowWaves};
+}
 
 // Rows of `part`: blocks that walk rows; of the wide form, the blocks that
 // share a tile of columns (8 blocks to a CU over all tiles).
-static int norm_grad_parts(int64_t rows, int64_t cols) {
-  const RowForm f = grad_form(cols);
+static int norm_grad_parts(bool bf16, int64_t rows, int64_t cols) {
+  const RowForm f = grad_form(bf16, cols);
   if (f.spans != 0) return static_cast<int>(row_blocks(f, rows));
   const int64_t tiles = (cols + kRowWaves * kSpanCols - 1) / (kRowWaves * kSpanCols);
   const int64_t want = tiles < 2048 ? 2048 / tiles : 1;
   return static_cast<int>(rows < want ? rows : want);
 }
 
-size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols, bool sums) {
-  const size_t part = sums ? static_cast<size_t>(norm_grad_parts(rows, cols)) * 2 * cols : 0;
-  return (part + (grad_form(cols).spans == 0 ? 2 * static_cast<size_t>(rows) : 0)) * sizeof(float);
+size_t norm_grad_workspace_bytes(bool bf16, int64_t rows, int64_t cols, bool sums) {
+  const size_t part = sums ? static_cast<size_t>(norm_grad_parts(bf16, rows, cols)) * 2 * cols : 0;
+  return (part + (grad_form(bf16, cols).spans == 0 ? 2 * static_cast<size_t>(rows) : 0)) *
+         sizeof(float);
 }
 
 template <typename T, bool ENDS>
 static hipError_t launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, float* part, float* means,
                                int parts, hipStream_t stream) {
-  const RowForm f = grad_form(a.cols);
+  const RowForm f = grad_form(sizeof(T) == 2, a.cols);
   const dim3 grid(parts), block(f.lanes <= kWave ? kRowThreads : f.lanes);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop, part);
@@ -813,9 +835,11 @@ static hipError_t launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, fl
                        stream, a, drop, means, part);
     return hipGetLastError();
   }
-  if (f.lanes > kWave)
-    return f.spans == 1 ? launch(norm_grad_block_kernel<T, 1024, ENDS, 1>)
-                        : launch(norm_grad_block_kernel<T, 512, ENDS, 2>);
+  if constexpr (sizeof(T) == 2) {
+    if (f.lanes > kWave && f.spans == 2)
+      return launch(norm_grad_block_kernel<T, kGradWaves2 * kWave, ENDS, 2>);
+  }
+  if (f.lanes > kWave) return launch(norm_grad_block_kernel<T, 1024, ENDS, 1>);
   switch (f.lanes * f.spans) {
     case 1: return launch(norm_grad_group_kernel<T, 1, ENDS, 1>);
     case 2: return launch(norm_grad_group_kernel<T, 2, ENDS, 1>);
@@ -833,7 +857,7 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& dro
   NormGradArgs a = args;
   a.stream = streams(bf16, a.rows, a.cols);
   const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
-  const int parts = norm_grad_parts(a.rows, a.cols);
+  const int parts = norm_grad_parts(bf16, a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;
   float* means = static_cast<float*>(workspace) + (sums ? static_cast<size_t>(parts) * 2 * a.cols : 0);
   hipError_t e = by_row_type(bf16, a.cols, [&](auto t, auto ends) {

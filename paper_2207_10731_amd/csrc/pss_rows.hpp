@@ -478,7 +478,7 @@ hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, co
 hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream);
 // workspace: norm_grad_workspace_bytes (may be 0); sums: a weight or bias gradient
 // is wanted.
-size_t norm_grad_workspace_bytes(int64_t rows, int64_t cols, bool sums);
+size_t norm_grad_workspace_bytes(bool bf16, int64_t rows, int64_t cols, bool sums);
 hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, void* workspace,
                             hipStream_t stream);
 

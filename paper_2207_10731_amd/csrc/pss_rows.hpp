@@ -191,11 +191,10 @@ __device__ __forceinline__ h8_any load_end(const uint16_t* p, int rest) {
 template <End E, typename T>
 __device__ __forceinline__ typename Vec<T>::type load_vec(const T* p, int n, int rest) {
   typedef typename Vec<T>::type V;
-  if (E == End::kWhole ? n > 0 : n >= kVec<T>)
+  if (E == End::kOverlap && n < kVec<T>) p += rest - kVec<T>;
+  if (E == End::kPieces ? n >= kVec<T> : n > 0)
     return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
   V x = 0;
-  if (E == End::kOverlap && n > 0)
-    x = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + rest - kVec<T>));
   if (E == End::kPieces && n > 0) x = load_end(p, rest);
   return x;
 }

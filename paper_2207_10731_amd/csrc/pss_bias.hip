@@ -30,10 +30,30 @@ __device__ __forceinline__ int key_rest(int64_t K) {
   return static_cast<int>(K) & (kVec<T> - 1);
 }
 
+// Buckets of the differences key - query that need no search: beyond the last
+// border, and ahead of the query on a single side.
+struct FarBuckets {
+  int behind, ahead;        // of differences <= -near, >= from
+  int32_t near, from;
+};
+__device__ __forceinline__ FarBuckets far_buckets(const BucketMap& map) {
+  FarBuckets f;
+  f.near = map.borders[map.side - 1];
+  f.behind = map.side - 1;
+  f.from = map.both ? (f.near > 1 ? f.near : 1) : 0;
+  f.ahead = map.num - 1;
+  if (!map.both) {  // the last of the buckets from distance 0 on
+    f.ahead = 0;
+    while (f.ahead + 1 < map.side && map.borders[f.ahead + 1] <= 0) ++f.ahead;
+  }
+  return f;
+}
+
 // ---------------------------------------------------------------------------
 // Forward, few queries (new tokens): 16 bytes of keys a lane.  Buckets are
-// ranges of distances, so keys whose ends share one (nearly all of a long cache)
-// need two searches, not one each.
+// ranges of distances: keys beyond the last border (nearly all of a long cache)
+// need no search, and keys whose ends share a bucket two, not one each.  A
+// wavefront copies the borders to LDS only if it has others.
 // ---------------------------------------------------------------------------
 template <typename T, bool ENDS>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
@@ -42,28 +62,40 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
                                                                 const uint32_t per) {
   constexpr int V = kVec<T>;
   constexpr End kEnd = ENDS ? End::kPieces : End::kWhole;
-  __shared__ int32_t borders[kMaxBuckets];
+  __shared__ int32_t all_borders[kBiasWaves][kMaxBuckets];
   const int rest = key_rest<T>(a.K);
-  for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
-  __syncthreads();
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
   const int64_t k = (static_cast<int64_t>(blockIdx.x % k_tiles) * tx + x) * V;
   const uint32_t row = tile_of(per, k_tiles) * (kBiasThreads / tx) + y;
-  if (k >= a.K || row >= static_cast<uint32_t>(a.B * a.H * a.Q)) return;
+  const bool mine = k < a.K && row < static_cast<uint32_t>(a.B * a.H * a.Q);
   const uint32_t bh = row / static_cast<uint32_t>(a.Q), q = row - bh * static_cast<uint32_t>(a.Q);
   const uint32_t b = bh / static_cast<uint32_t>(a.H), h = bh - b * static_cast<uint32_t>(a.H);
-  const int len = keys_left(k, a.K);
+  const int len = mine ? keys_left(k, a.K) : 0;
   float v[V];
   typename Vec<T>::type raw;
   if (a.in != nullptr)
     raw = load_vec<kEnd>(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
                              q * a.in_stride[2] + k, len, rest);
-  const int32_t rel = static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q);
-  const int j0 = bucket_of(rel, borders, map.side, map.both);
-  const int j1 = bucket_of(rel + V - 1, borders, map.side, map.both);
-  // behind the query buckets fall with the key, ahead of it they rise: equal
-  // ends on one side of it hold all between
-  if (j0 == j1 && (rel >= 0 || rel + V - 1 <= 0)) {
+  const FarBuckets far = far_buckets(map);
+  const int32_t rel = mine ? static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q)
+                           : far.from;
+  const bool is_behind = rel + V - 1 <= -far.near, is_far = is_behind || rel >= far.from;
+  int j0 = is_behind ? far.behind : far.ahead;
+  bool one = true;
+  int32_t* borders = all_borders[threadIdx.x >> 6];
+  if (__any(!is_far)) {
+    for (int i = threadIdx.x & (kWave - 1); i < map.side; i += kWave) borders[i] = map.borders[i];
+    wave_lds_fence();
+    if (!is_far) {
+      j0 = bucket_of(rel, borders, map.side, map.both);
+      // behind the query buckets fall with the key, ahead of it they rise: equal
+      // ends on one side of it hold all between
+      one = j0 == bucket_of(rel + V - 1, borders, map.side, map.both) &&
+            (rel >= 0 || rel + V - 1 <= 0);
+    }
+  }
+  if (!mine) return;
+  if (one) {
     const float t = table_entry(a, j0 * a.H + h);
 #pragma unroll
     for (int u = 0; u < V; ++u) v[u] = t;
@@ -89,11 +121,9 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
 // The first scores are on their way meanwhile.  Short sequences: a block takes
 // several (batch, head) pairs, a window of differences to each.
 // ---------------------------------------------------------------------------
-constexpr int kStep = 8;      // queries a lane takes at a time
-constexpr int kMaxSteps = 4;
+constexpr int kStep = 8;  // queries of a lane
 
 struct BiasTile {
-  int steps;         // a group's, of 8 queries each
   uint32_t pairs;    // (batch, head) pairs of a block
   uint32_t groups;   // of lanes to a pair
   uint32_t q_tiles;  // of a pair
@@ -106,16 +136,15 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
                                                                  const BucketMap map,
                                                                  const BiasTile tl) {
   constexpr int V = kVec<T>, TY = kBiasThreads / TX, kKeys = TX * V;
-  constexpr int kOne = kKeys + kMaxSteps * TY * kStep, kMany = TY * (kKeys + kStep);
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float column[kMaxBuckets];
-  __shared__ float windows[kOne > kMany ? kOne : kMany];
+  __shared__ float windows[TY * (kKeys + kStep)];
   const uint32_t tile = tile_of(tl.per, tl.k_tiles), kt = blockIdx.x % tl.k_tiles;
   const uint32_t pt = tile / tl.q_tiles, qt = tile - pt * tl.q_tiles;
   const uint32_t H = static_cast<uint32_t>(a.H), all = static_cast<uint32_t>(a.B * a.H);
   const uint32_t bh0 = pt * tl.pairs;
   if (bh0 >= all) return;
-  const int rows = tl.steps * static_cast<int>(tl.groups) * kStep;  // of a pair's tile
+  const int rows = static_cast<int>(tl.groups) * kStep;  // of a pair's tile
   const int64_t q0 = static_cast<int64_t>(qt) * rows, k0 = static_cast<int64_t>(kt) * kKeys;
   const int x = threadIdx.x % TX;
   const uint32_t y = threadIdx.x / TX;
@@ -125,13 +154,14 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
   const int64_t k = k0 + x * V;
   const int len = mine ? keys_left(k, a.K) : 0;
   const int rest = key_rest<T>(a.K);
-  int row = static_cast<int>(y - pair * tl.groups) * kStep;
+  const int row = static_cast<int>(y - pair * tl.groups) * kStep;
+  const int64_t q = q0 + row;
   const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] + k;
   typename Vec<T>::type raw[kStep];
   if (a.in != nullptr) {
 #pragma unroll
     for (int j = 0; j < kStep; ++j)
-      raw[j] = load_vec<E>(in + (q0 + row + j) * a.in_stride[2], q0 + row + j < a.Q ? len : 0, rest);
+      raw[j] = load_vec<E>(in + (q + j) * a.in_stride[2], q + j < a.Q ? len : 0, rest);
   }
   for (int i = threadIdx.x; i < map.num; i += kBiasThreads) {
     if (i < map.side) borders[i] = map.borders[i];
@@ -141,57 +171,57 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
   const int size = kKeys + rows;  // of a window, with one more than it needs
   // difference of its first entry: the tile's first key, its last query
   const int32_t rel0 = static_cast<int32_t>(k0 - q0 - (rows - 1));
+  const FarBuckets far = far_buckets(map);
+  const auto bucket = [&](int32_t rel) {
+    if (rel <= -far.near) return far.behind;
+    return rel >= far.from ? far.ahead : bucket_of(rel, borders, map.side, map.both);
+  };
   if (tl.pairs == 1) {
     const int32_t rel = rel0 - first_position(a, b);
-    for (int i = threadIdx.x; i < size - 1; i += kBiasThreads)
-      windows[i] = column[bucket_of(rel + i, borders, map.side, map.both)];
+    for (int i = threadIdx.x; i < size - 1; i += kBiasThreads) windows[i] = column[bucket(rel + i)];
   } else {
     for (uint32_t i = threadIdx.x; i < tl.pairs * size; i += kBiasThreads) {
       const uint32_t w = i / size, bh1 = bh0 + w, b1 = bh1 / H;
       if (bh1 >= all) break;
       const int32_t rel = rel0 - first_position(a, b1) + static_cast<int32_t>(i - w * size);
-      windows[i] = table_entry(
-          a, static_cast<int64_t>(bucket_of(rel, borders, map.side, map.both)) * a.H + bh1 - b1 * H);
+      windows[i] = table_entry(a, static_cast<int64_t>(bucket(rel)) * a.H + bh1 - b1 * H);
     }
   }
   __syncthreads();
-  if (len <= 0) return;
+  if (len <= 0 || q >= a.Q) return;
   const float* window = windows + pair * size;
   T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] + k;
-  for (int s = 0; s < tl.steps; ++s, row += static_cast<int>(tl.groups) * kStep) {
-    const int64_t q = q0 + row;
-    if (q >= a.Q) return;
-    if (a.in != nullptr && s > 0) {
+  // bias of query q + j and key k + u: near[7 + u - j]
+  const int at = x * V + rows - 1 - row - (kStep - 1);
+  float near[V + kStep - 1];
 #pragma unroll
-      for (int j = 0; j < kStep; ++j)
-        if (q + j < a.Q) raw[j] = load_vec<E>(in + (q + j) * a.in_stride[2], len, rest);
+  for (int i = 0; i < V + kStep - 1; ++i) near[i] = window[at + i];
+#pragma unroll
+  for (int j = 0; j < kStep; ++j) {
+    if (q + j >= a.Q) break;
+    float v[V];
+    if (a.in != nullptr) raw[j] = settle<E>(raw[j], len, rest);
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      v[u] = near[kStep - 1 + u - j];
+      if (a.in != nullptr) v[u] += widen(raw[j][u]);
     }
-    // bias of query q + j and key k + u: near[7 + u - j]
-    const int at = x * V + rows - 1 - row - (kStep - 1);
-    float near[V + kStep - 1];
-#pragma unroll
-    for (int i = 0; i < V + kStep - 1; ++i) near[i] = window[at + i];
-#pragma unroll
-    for (int j = 0; j < kStep; ++j) {
-      if (q + j >= a.Q) break;
-      float v[V];
-      if (a.in != nullptr) raw[j] = settle<E>(raw[j], len, rest);
-#pragma unroll
-      for (int u = 0; u < V; ++u) {
-        v[u] = near[kStep - 1 + u - j];
-        if (a.in != nullptr) v[u] += widen(raw[j][u]);
-      }
-      store_vec<E != End::kWhole>(out + (q + j) * a.out_stride[2], v, len, a.stream);
-    }
+    store_vec<E != End::kWhole>(out + (q + j) * a.out_stride[2], v, len, a.stream);
   }
 }
 
-// Lanes along the keys, `vec` keys each: as many as there are keys, `least` to a
-// whole block.
-static int key_lanes(int64_t K, int vec, int least) {
+// Lanes along the keys, `vec` keys each, `least` to `most`: as many as there are
+// keys, but several tiles of fewer lanes where more than an eighth of the lanes
+// would have none (511 x 517 bfloat16, 65 vectors in tiles of 16 lanes instead of
+// 128).
+static int key_lanes(int64_t K, int vec, int least, int most) {
   const int64_t pieces = (K + vec - 1) / vec;
   int tx = least;
-  while (tx < pieces && tx < kBiasThreads) tx *= 2;
+  while (tx < pieces && tx < most) tx *= 2;
+  const auto lanes = [&](int t) { return (pieces + t - 1) / t * t; };
+  int64_t fewest = lanes(tx);
+  for (int t = tx / 2; t >= 16 && t >= least; t /= 2) fewest = lanes(t) < fewest ? lanes(t) : fewest;
+  while (lanes(tx) > fewest + fewest / 8) tx /= 2;
   return tx;
 }
 
@@ -207,7 +237,7 @@ static auto with_lanes(int n, F f) {
 template <typename T>
 static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
   const dim3 block(kBiasThreads);
-  const int tx = key_lanes(a.K, kVec<T>, 4), ty = kBiasThreads / tx;
+  const int tx = key_lanes(a.K, kVec<T>, 4, kBiasThreads), ty = kBiasThreads / tx;
   const int64_t keys = static_cast<int64_t>(tx) * kVec<T>;
   const int64_t k_tiles = (a.K + keys - 1) / keys, bh = a.B * a.H;
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
@@ -222,7 +252,6 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
     return a.K % kVec<T> ? launch(bias_row_kernel<T, true>) : launch(bias_row_kernel<T, false>);
   }
   BiasTile tl;
-  tl.steps = 1;
   tl.pairs = 1;
   tl.groups = ty;
   int64_t q_tiles = 1;
@@ -230,13 +259,9 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
   if (k_tiles == 1 && 2 * q_steps <= ty) {
     tl.groups = static_cast<uint32_t>(q_steps);
     tl.pairs = ty / tl.groups;
-    while (tl.pairs > 1 && bh < 2048 * static_cast<int64_t>(tl.pairs)) tl.pairs /= 2;
+    while (tl.pairs > 1 && bh < 512 * static_cast<int64_t>(tl.pairs)) tl.pairs /= 2;
   } else {
-    // as many queries to a block as leave 8 blocks to a CU
-    tl.steps = kMaxSteps;
-    while (tl.steps > 1 && bh * k_tiles * ((q_steps + ty * tl.steps - 1) / (ty * tl.steps)) < 2048)
-      tl.steps /= 2;
-    q_tiles = (q_steps + ty * tl.steps - 1) / (ty * tl.steps);
+    q_tiles = (q_steps + ty - 1) / ty;
   }
   const int64_t tiles = (bh + tl.pairs - 1) / tl.pairs * q_tiles;
   const TileGrid tg = tile_grid(tiles, k_tiles);
@@ -256,8 +281,7 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
     // unless it is the first one
     if (a.K / kVec<T> % (TX < kWave ? TX : kWave) != 0)
       return launch(bias_tile_kernel<T, TX, End::kOverlap>);
-    if constexpr (TX == 4 || TX >= kWave) return launch(bias_tile_kernel<T, TX, End::kPieces>);
-    return hipErrorInvalidValue;  // not reached: TX of 8 to 32 has more than TX / 2 vectors
+    return launch(bias_tile_kernel<T, TX, End::kPieces>);
   });
 }
 
@@ -333,9 +357,7 @@ static bool is_near(const BucketMap& map) { return map.borders[map.side - 1] <= 
 static NearShape near_shape(bool bf16, const BiasArgs& a, const BucketMap& map) {
   NearShape s;
   const int vec = bf16 ? kVec<uint16_t> : kVec<float>;
-  const int64_t pieces = (a.K + vec - 1) / vec;
-  s.tx = 8;
-  while (s.tx < pieces && s.tx < kWave) s.tx *= 2;
+  s.tx = key_lanes(a.K, vec, 8, kWave);
   s.qu = kStep;
   while (s.qu > 1 && s.qu / 2 >= a.Q) s.qu /= 2;
   const int64_t keys = static_cast<int64_t>(s.tx) * vec * (kStep / s.qu);
@@ -479,8 +501,7 @@ struct FarShape {
 static FarShape far_shape(bool bf16, const BiasArgs& a) {
   FarShape s;
   const int vec = bf16 ? kVec<uint16_t> : kVec<float>;
-  s.tx = key_lanes(a.K, vec, 16);
-  if (s.tx > kWave) s.tx = kWave;
+  s.tx = key_lanes(a.K, vec, 16, kWave);
   const int groups = kBiasThreads / s.tx;
   const int64_t keys = static_cast<int64_t>(s.tx) * vec;
   s.k_tiles = (a.K + keys - 1) / keys;

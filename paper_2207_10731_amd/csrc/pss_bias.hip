@@ -1,7 +1,5 @@
 // Learned relative position bias by buckets: scores + table[bucket], and the
 // table's gradient.
-#include <type_traits>
-
 #include "pss_rows.hpp"
 
 namespace pss {
@@ -55,7 +53,7 @@ __device__ __forceinline__ FarBuckets far_buckets(const BucketMap& map) {
 // need no search, and keys whose ends share a bucket two, not one each.  A
 // wavefront copies the borders to LDS only if it has others.
 // ---------------------------------------------------------------------------
-template <typename T, bool ENDS>
+template <typename T, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
                                                                 const BucketMap map, const int tx,
                                                                 const uint32_t k_tiles,
@@ -109,8 +107,8 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
 #pragma unroll
     for (int u = 0; u < V; ++u) v[u] += widen(raw[u]);
   }
-  store_vec<ENDS>(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
-                      q * a.out_stride[2] + k, v, len, a.stream);
+  store_vec<ENDS, PAST>(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
+                            q * a.out_stride[2] + k, v, len);
 }
 
 // ---------------------------------------------------------------------------
@@ -131,7 +129,7 @@ struct BiasTile {
   uint32_t per;      // tile_of
 };
 
-template <typename T, int TX, End E>
+template <typename T, int TX, End E, bool PAST>
 __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs a,
                                                                  const BucketMap map,
                                                                  const BiasTile tl) {
@@ -206,7 +204,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
       v[u] = near[kStep - 1 + u - j];
       if (a.in != nullptr) v[u] += widen(raw[j][u]);
     }
-    store_vec<E != End::kWhole>(out + (q + j) * a.out_stride[2], v, len, a.stream);
+    store_vec<E != End::kWhole, PAST>(out + (q + j) * a.out_stride[2], v, len);
   }
 }
 
@@ -225,13 +223,10 @@ static int key_lanes(int64_t K, int vec, int least, int most) {
   return tx;
 }
 
-// f(the constant that n equals); n is one of them.
-template <int N, int... MORE, typename F>
-static auto with_lanes(int n, F f) {
-  if constexpr (sizeof...(MORE) > 0) {
-    if (n != N) return with_lanes<MORE...>(n, f);
-  }
-  return f(std::integral_constant<int, N>{});
+// launch(whether the results go past the caches)
+template <typename F>
+static hipError_t by_store(bool past, F launch) {
+  return past ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 template <typename T>
@@ -240,6 +235,10 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
   const int tx = key_lanes(a.K, kVec<T>, 4, kBiasThreads), ty = kBiasThreads / tx;
   const int64_t keys = static_cast<int64_t>(tx) * kVec<T>;
   const int64_t k_tiles = (a.K + keys - 1) / keys, bh = a.B * a.H;
+  // (several narrow bfloat16 rows to a wavefront that are not whole lines: 9% slower
+  // past the caches)
+  const bool past = bh * a.Q * a.K * static_cast<int64_t>(sizeof(T)) > kPastBytes &&
+                    (sizeof(T) == 4 || tx >= kWave || a.K % 32 == 0);
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
     const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
     const TileGrid tg = tile_grid(row_tiles, k_tiles);
@@ -249,7 +248,10 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
                          static_cast<uint32_t>(k_tiles), tg.per);
       return hipGetLastError();
     };
-    return a.K % kVec<T> ? launch(bias_row_kernel<T, true>) : launch(bias_row_kernel<T, false>);
+    return by_store(past, [&](auto to) {
+      return a.K % kVec<T> ? launch(bias_row_kernel<T, true, to.value>)
+                           : launch(bias_row_kernel<T, false, to.value>);
+    });
   }
   BiasTile tl;
   tl.pairs = 1;
@@ -274,23 +276,20 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
     hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, tl);
     return hipGetLastError();
   };
-  return with_lanes<4, 8, 16, 32, 64, 128, 256>(tx, [&](auto lanes) {
+  return with_const<4, 8, 16, 32, 64, 128, 256>(tx, [&](auto lanes) {
     constexpr int TX = lanes.value;
-    if (a.K % kVec<T> == 0) return launch(bias_tile_kernel<T, TX, End::kWhole>);
-    // the lane with a row's end has the elements before it in its own wavefront,
-    // unless it is the first one
-    if (a.K / kVec<T> % (TX < kWave ? TX : kWave) != 0)
-      return launch(bias_tile_kernel<T, TX, End::kOverlap>);
-    return launch(bias_tile_kernel<T, TX, End::kPieces>);
+    return by_store(past, [&](auto to) {
+      if (a.K % kVec<T> == 0) return launch(bias_tile_kernel<T, TX, End::kWhole, to.value>);
+      // the lane with a row's end has the elements before it in its own wavefront,
+      // unless it is the first one
+      if (a.K / kVec<T> % (TX < kWave ? TX : kWave) != 0)
+        return launch(bias_tile_kernel<T, TX, End::kOverlap, to.value>);
+      return launch(bias_tile_kernel<T, TX, End::kPieces, to.value>);
+    });
   });
 }
 
-// Results of more than this are stored past the caches.
-constexpr int64_t kStreamBytes = int64_t{32} << 20;
-
-hipError_t launch_bias(bool bf16, const BiasArgs& args, const BucketMap& map, hipStream_t stream) {
-  BiasArgs a = args;
-  a.stream = a.B * a.H * a.Q * a.K * (bf16 ? 2 : 4) > kStreamBytes;
+hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipStream_t stream) {
   return bf16 ? launch_bias_t<uint16_t>(a, map, stream) : launch_bias_t<float>(a, map, stream);
 }
 
@@ -644,12 +643,12 @@ static hipError_t launch_near(const BiasArgs& a, const BucketMap& map, const Nea
     return hipGetLastError();
   };
   return by_key_end<T>(a.K, [&](auto end) {
-    return with_lanes<8, 16, 32, 64>(s.tx, [&](auto lanes) {
+    return with_const<8, 16, 32, 64>(s.tx, [&](auto lanes) {
       constexpr End E = end.value;
       if constexpr (E == End::kPieces && lanes.value != 8) {
         return hipErrorInvalidValue;  // not reached: less than a vector of keys has 8 lanes
       } else {
-        return with_lanes<1, 2, 4, 8>(s.qu, [&](auto qu) {
+        return with_const<1, 2, 4, 8>(s.qu, [&](auto qu) {
           return launch(bias_grad_near_kernel<T, lanes.value, qu.value, E>);
         });
       }
@@ -666,7 +665,7 @@ static hipError_t launch_far(const BiasArgs& a, const BucketMap& map, const FarS
     return hipGetLastError();
   };
   return by_key_end<T>(a.K, [&](auto end) {
-    return with_lanes<16, 32, 64>(s.tx, [&](auto lanes) {
+    return with_const<16, 32, 64>(s.tx, [&](auto lanes) {
       constexpr End E = end.value;
       if constexpr (E == End::kPieces && lanes.value != 16) {
         return hipErrorInvalidValue;  // not reached: less than a vector of keys has 16 lanes

@@ -1,7 +1,5 @@
 // Operators on rows: dropout from a counter-based generator, layer norm and
 // its backward pass.
-#include <type_traits>
-
 #include "pss_rows.hpp"
 
 namespace pss {
@@ -44,13 +42,12 @@ static hipError_t by_row_type(bool bf16, int64_t cols, F f) {
 // ---------------------------------------------------------------------------
 // out = residual + D(x): a span of a row to a group of G lanes.
 // ---------------------------------------------------------------------------
-template <typename T, int G, bool ENDS>
+template <typename T, int G, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, const RowsIn residual,
                                                               const RowsOut out, const int64_t rows,
                                                               const int64_t cols,
                                                               const uint32_t spans,
-                                                              const uint32_t per, const Drop drop,
-                                                              const bool stream) {
+                                                              const uint32_t per, const Drop drop) {
   typedef Span<T, G, ENDS> S;
   const uint64_t n = drop.t ? drop_offset(drop) : 0;
   const uint32_t tile = tile_of(per, spans), span = blockIdx.x % spans;
@@ -74,13 +71,22 @@ __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, co
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) v[u] += q[u];
   }
-  S::store(static_cast<T*>(out.p) + r * out.stride + c, v, lane, left, stream);
+  S::template store<PAST>(static_cast<T*>(out.p) + r * out.stride + c, v, lane, left);
 }
 
-// Results of more than this are stored past the caches.
-constexpr int64_t kStreamBytes = int64_t{32} << 20;
-static bool streams(bool bf16, int64_t rows, int64_t cols) {
-  return rows * cols * (bf16 ? 2 : 4) > kStreamBytes;
+// Kernels whose stores gain past the caches: those of whole lines, which a
+// wavefront's bfloat16 rows fill and float32 ones (in two stores, a span's halves)
+// if they are wide (norm of 1048576 x 16 float32: 40 us past them, 32 through
+// them; of 524288 x 64: 47 and 50).
+template <typename T, int G, bool ENDS>
+constexpr bool kGainsPast = sizeof(T) == 2 || G == kWave || (!ENDS && G >= 8);
+// launch(whether the results go past the caches)
+template <typename T, int G, bool ENDS, typename F>
+static hipError_t by_store(int64_t elements, F launch) {
+  if constexpr (kGainsPast<T, G, ENDS>) {
+    if (elements * static_cast<int64_t>(sizeof(T)) > kPastBytes) return launch(std::true_type{});
+  }
+  return launch(std::false_type{});
 }
 
 template <typename T, bool ENDS>
@@ -92,21 +98,17 @@ static hipError_t launch_dropout_t(const RowsIn& x, const RowsIn& residual, cons
   const int64_t tiles = (rows * g + kRowThreads - 1) / kRowThreads;
   const TileGrid tg = tile_grid(tiles, spans);
   if (!tg.fits) return hipErrorInvalidConfiguration;
-  const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, tg.grid, dim3(kRowThreads), 0, stream, x, residual, out, rows, cols,
-                       static_cast<uint32_t>(spans), tg.per, drop,
-                       streams(sizeof(T) == 2, rows, cols));
-    return hipGetLastError();
-  };
-  switch (g) {
-    case 1: return launch(dropout_kernel<T, 1, ENDS>);
-    case 2: return launch(dropout_kernel<T, 2, ENDS>);
-    case 4: return launch(dropout_kernel<T, 4, ENDS>);
-    case 8: return launch(dropout_kernel<T, 8, ENDS>);
-    case 16: return launch(dropout_kernel<T, 16, ENDS>);
-    case 32: return launch(dropout_kernel<T, 32, ENDS>);
-    default: return launch(dropout_kernel<T, 64, ENDS>);
-  }
+  // (float32 with a residual: 3 to 6% slower past the caches)
+  const int64_t stored = sizeof(T) == 4 && residual.p != nullptr ? 0 : rows * cols;
+  return with_const<1, 2, 4, 8, 16, 32, 64>(g, [&](auto lanes) {
+    constexpr int G = lanes.value;
+    return by_store<T, G, ENDS>(stored, [&](auto past) {
+      hipLaunchKernelGGL((dropout_kernel<T, G, ENDS, past.value>), tg.grid, dim3(kRowThreads), 0,
+                         stream, x, residual, out, rows, cols, static_cast<uint32_t>(spans), tg.per,
+                         drop);
+      return hipGetLastError();
+    });
+  });
 }
 
 hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, const RowsOut& out,
@@ -152,16 +154,16 @@ struct NormSpan {
   }
 };
 
-template <typename T, int G, bool ENDS>
+template <typename T, int G, bool ENDS, bool PAST>
 __device__ __forceinline__ void norm_store(float v[kLanePiece], const NormArgs& a, int64_t r,
                                            int64_t c, int lane, int left, float mean, float rstd,
                                            const float w[kLanePiece], const float b[kLanePiece]) {
   typedef Span<T, G, ENDS> S;
   if (a.sum.p != nullptr)
-    S::store(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v, lane, left, a.stream);
+    S::template store<PAST>(static_cast<T*>(a.sum.p) + r * a.sum.stride + c, v, lane, left);
 #pragma unroll
   for (int u = 0; u < kLanePiece; ++u) v[u] = (v[u] - mean) * rstd * w[u] + b[u];
-  S::store(static_cast<T*>(a.out.p) + r * a.out.stride + c, v, lane, left, a.stream);
+  S::template store<PAST>(static_cast<T*>(a.out.p) + r * a.out.stride + c, v, lane, left);
 }
 
 __device__ __forceinline__ void norm_store_stats(const NormArgs& a, int64_t r, float mean,
@@ -185,7 +187,7 @@ __device__ __forceinline__ float squares(const float v[kLanePiece], int lane, in
 
 // A group of G lanes a row, NP spans.  AHEAD: the next row is requested before the
 // present one's sums.  (4 wavefronts to a SIMD: at most 128 registers.)
-template <typename T, int G, bool ENDS, int NP, bool AHEAD>
+template <typename T, int G, bool ENDS, bool PAST, int NP, bool AHEAD>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_group_kernel(const NormArgs a, const Drop drop) {
   constexpr int kRows = kRowThreads / G, kSpan = G * kLanePiece;
   const int lane = threadIdx.x % G;
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void norm_group_kernel(const NormAr
       if (lane == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
       for (int i = 0; i < NP; ++i)
-        norm_store<T, G, ENDS>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
+        norm_store<T, G, ENDS, PAST>(v[i], a, r, i * kSpan, lane, cols - i * kSpan, mean, rstd, w[i], b[i]);
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
@@ -252,7 +254,7 @@ __device__ __forceinline__ float part_size(int k, int n, int cols) {
 // parts are joined through LDS with one barrier a row (the squares about the
 // common mean are those about each part's plus the part's size times the square
 // of its mean's distance).
-template <typename T, int TH, bool ENDS, int NP, bool AHEAD>
+template <typename T, int TH, bool ENDS, bool PAST, int NP, bool AHEAD>
 __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2][2][kMaxWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = group_of<kWave>();
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, con
     if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      norm_store<T, kWave, ENDS>(v[i], a, r, c[i], lane, cols - c[i], mean, rstd, w[i], b[i]);
+      norm_store<T, kWave, ENDS, PAST>(v[i], a, r, c[i], lane, cols - c[i], mean, rstd, w[i], b[i]);
       if (AHEAD)
         in[i] = next[i];
       else if (after < a.rows)
@@ -338,7 +340,7 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
 // Wider rows: a block a row, which it reads three times (sum, squares about the
 // mean, result), the last two from L2.  Nothing is stored before the last pass,
 // where every element is read by the lane that then stores its results.
-template <typename T, bool ENDS>
+template <typename T, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2 * kRowWaves];
   const int lane = threadIdx.x & (kWave - 1);
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArg
       in.sum_to(v, a, drop, n, r, c, lane, left);
       Span<T, kWave, ENDS>::weights(w, a.weight, a.weight_bf16, c, lane, left, 1.f);
       Span<T, kWave, ENDS>::weights(b, a.bias, a.weight_bf16, c, lane, left, 0.f);
-      norm_store<T, kWave, ENDS>(v, a, r, c, lane, left, mean, rstd, w, b);
+      norm_store<T, kWave, ENDS, PAST>(v, a, r, c, lane, left, mean, rstd, w, b);
     }
   }
 }
@@ -437,27 +439,27 @@ static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop);
     return hipGetLastError();
   };
-  if (f.spans == 0) return launch(norm_wide_kernel<T, ENDS>);
-  if (f.lanes > kWave) {
-    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, ENDS, 1, true>);
-    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, ENDS, 2, kAhead2>)
-                          : launch(norm_block_kernel<T, 1024, ENDS, 2, false>);
+  if (f.lanes < kWave) {
+    return with_const<1, 2, 4, 8, 16, 32>(f.lanes, [&](auto lanes) {
+      constexpr int G = lanes.value;
+      return by_store<T, G, ENDS>(a.rows * a.cols, [&](auto past) {
+        return launch(norm_group_kernel<T, G, ENDS, past.value, 1, true>);
+      });
+    });
   }
-  switch (f.lanes * f.spans) {
-    case 1: return launch(norm_group_kernel<T, 1, ENDS, 1, true>);
-    case 2: return launch(norm_group_kernel<T, 2, ENDS, 1, true>);
-    case 4: return launch(norm_group_kernel<T, 4, ENDS, 1, true>);
-    case 8: return launch(norm_group_kernel<T, 8, ENDS, 1, true>);
-    case 16: return launch(norm_group_kernel<T, 16, ENDS, 1, true>);
-    case 32: return launch(norm_group_kernel<T, 32, ENDS, 1, true>);
-    case 64: return launch(norm_group_kernel<T, 64, ENDS, 1, true>);
-    default: return launch(norm_group_kernel<T, 64, ENDS, 2, kAhead2>);
-  }
+  return by_store<T, kWave, ENDS>(a.rows * a.cols, [&](auto past) {
+    constexpr bool PAST = past.value;
+    if (f.spans == 0) return launch(norm_wide_kernel<T, ENDS, PAST>);
+    if (f.lanes == kWave)
+      return f.spans == 1 ? launch(norm_group_kernel<T, kWave, ENDS, PAST, 1, true>)
+                          : launch(norm_group_kernel<T, kWave, ENDS, PAST, 2, kAhead2>);
+    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, ENDS, PAST, 1, true>);
+    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, ENDS, PAST, 2, kAhead2>)
+                          : launch(norm_block_kernel<T, 1024, ENDS, PAST, 2, false>);
+  });
 }
 
-hipError_t launch_norm(bool bf16, const NormArgs& args, const Drop& drop, hipStream_t stream) {
-  NormArgs a = args;
-  a.stream = streams(bf16, a.rows, a.cols);
+hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream_t stream) {
   return by_row_type(bf16, a.cols, [&](auto t, auto ends) {
     return launch_norm_t<decltype(t), ends.value>(a, drop, stream);
   });
@@ -524,12 +526,12 @@ struct GradSpan {
       for (int u = 0; u < kLanePiece; ++u) d[u] += z[u];
     }
     if (a.grad_residual.p != nullptr)
-      S::store(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d, lane, left,
-               a.stream);
+      S::template store<false>(static_cast<T*>(a.grad_residual.p) + r * a.grad_residual.stride + c, d,
+                               lane, left);
     if (a.grad_x.p != nullptr) {
       if (drop.t)
         S::drop(d, drop, n, static_cast<uint32_t>(c / kLanePiece), static_cast<uint32_t>(r), lane);
-      S::store(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, lane, left, a.stream);
+      S::template store<false>(static_cast<T*>(a.grad_x.p) + r * a.grad_x.stride + c, d, lane, left);
     }
   }
 };
@@ -666,8 +668,8 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
   float* mine = part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    Span<T, kWave, ENDS>::store(mine + c[i], gw[i], lane, cols - c[i], false);
-    Span<T, kWave, ENDS>::store(mine + cols + c[i], gb[i], lane, cols - c[i], false);
+    Span<T, kWave, ENDS>::template store<false>(mine + c[i], gw[i], lane, cols - c[i]);
+    Span<T, kWave, ENDS>::template store<false>(mine + cols + c[i], gb[i], lane, cols - c[i]);
   }
 }
 
@@ -734,8 +736,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_tile_kernel(
   }
   if (part == nullptr) return;
   float* mine = part + static_cast<int64_t>(blockIdx.y) * 2 * a.cols + c;
-  Span<T, kWave, ENDS>::store(mine, gw, lane, left, false);
-  Span<T, kWave, ENDS>::store(mine + a.cols, gb, lane, left, false);
+  Span<T, kWave, ENDS>::template store<false>(mine, gw, lane, left);
+  Span<T, kWave, ENDS>::template store<false>(mine + a.cols, gb, lane, left);
 }
 
 // Sums the blocks' parts: 16 columns a block, 64 threads to each, which request
@@ -840,22 +842,14 @@ static hipError_t launch_norm_grad_t(const NormGradArgs& a, const Drop& drop, fl
       return launch(norm_grad_block_kernel<T, kGradWaves2 * kWave, ENDS, 2>);
   }
   if (f.lanes > kWave) return launch(norm_grad_block_kernel<T, 1024, ENDS, 1>);
-  switch (f.lanes * f.spans) {
-    case 1: return launch(norm_grad_group_kernel<T, 1, ENDS, 1>);
-    case 2: return launch(norm_grad_group_kernel<T, 2, ENDS, 1>);
-    case 4: return launch(norm_grad_group_kernel<T, 4, ENDS, 1>);
-    case 8: return launch(norm_grad_group_kernel<T, 8, ENDS, 1>);
-    case 16: return launch(norm_grad_group_kernel<T, 16, ENDS, 1>);
-    case 32: return launch(norm_grad_group_kernel<T, 32, ENDS, 1>);
-    case 64: return launch(norm_grad_group_kernel<T, 64, ENDS, 1>);
-    default: return launch(norm_grad_group_kernel<T, 64, ENDS, 2>);
-  }
+  if (f.spans == 2) return launch(norm_grad_group_kernel<T, kWave, ENDS, 2>);
+  return with_const<1, 2, 4, 8, 16, 32, 64>(f.lanes, [&](auto lanes) {
+    return launch(norm_grad_group_kernel<T, lanes.value, ENDS, 1>);
+  });
 }
 
-hipError_t launch_norm_grad(bool bf16, const NormGradArgs& args, const Drop& drop, void* workspace,
+hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, void* workspace,
                             hipStream_t stream) {
-  NormGradArgs a = args;
-  a.stream = streams(bf16, a.rows, a.cols);
   const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
   const int parts = norm_grad_parts(bf16, a.rows, a.cols);
   float* part = sums ? static_cast<float*>(workspace) : nullptr;

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "pss_kernels.hpp"
 
 namespace pss {
@@ -43,7 +45,6 @@ struct NormArgs {
   float* mean = nullptr;
   float* rstd = nullptr;
   int64_t rows = 0, cols = 0;
-  bool stream = false;  // results are stored past the caches (set by the launcher)
 };
 
 struct NormGradArgs {
@@ -56,7 +57,6 @@ struct NormGradArgs {
   float* grad_weight = nullptr;
   float* grad_bias = nullptr;
   int64_t rows = 0, cols = 0;
-  bool stream = false;  // as in NormArgs
 };
 
 // Position buckets: `num` in all, one side's `side` borders.
@@ -76,7 +76,6 @@ struct BiasArgs {
   int64_t out_stride[3] = {0, 0, 0};
   const void* table = nullptr;
   bool table_bf16 = false;
-  bool stream = false;  // as in NormArgs
 };
 
 // Bucket of a key `rel` positions ahead of its query (rel <= 0: behind it).
@@ -288,14 +287,14 @@ __device__ __forceinline__ void store_end(uint16_t* p, h8_any a, int n) {
   }
   if (n & 1) *p = static_cast<uint16_t>(w[0]);
 }
-// stream: past the caches (results too large for them); ENDS: n may be below kVec
-// and above 0.
-template <bool ENDS, typename T>
-__device__ __forceinline__ void store_vec(T* p, const float* v, int n, bool stream) {
+// PAST: past the caches; ENDS: n may be below kVec and above 0.  (PAST is a
+// kernel's own: of two kinds of store in one kernel the compiler makes one.)
+template <bool ENDS, bool PAST, typename T>
+__device__ __forceinline__ void store_vec(T* p, const float* v, int n) {
   typedef typename Vec<T>::type V;
   const V a = narrow(v, T{});
   if (ENDS ? n >= kVec<T> : n > 0) {
-    if (stream)
+    if constexpr (PAST)
       __builtin_nontemporal_store(a, reinterpret_cast<V*>(p));
     else
       *reinterpret_cast<V*>(p) = a;
@@ -350,13 +349,12 @@ struct Span {
 #pragma unroll
     for (int u = 0; u < kLanePiece; ++u) v[u] = widen(q[u / kVec<T>][u % kVec<T>]);
   }
-  template <typename O>
-  static __device__ __forceinline__ void store(O* p, const float v[kLanePiece], int lane, int left,
-                                               bool stream) {
+  template <bool PAST, typename O>
+  static __device__ __forceinline__ void store(O* p, const float v[kLanePiece], int lane, int left) {
     constexpr int V = kVec<O> < kVec<T> ? kVec<O> : kVec<T>;  // consecutive columns
 #pragma unroll
     for (int u = 0; u < kLanePiece; u += V)
-      store_vec<ENDS>(p + col(lane, u), v + u, left - col(lane, u), stream);
+      store_vec<ENDS, PAST>(p + col(lane, u), v + u, left - col(lane, u));
   }
   // Weights (bf16: their storage) from column c0 on in the span's layout; null:
   // `fill`.  Other blocks read them too: through the caches, in fours.
@@ -442,6 +440,21 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
+
+// Results of more than this are stored past the caches where that is faster: alone,
+// bias of 2 x 16 x 2048 x 2048 bfloat16 88 against 94 us, norm of 16384 x 4096
+// 50 against 54 with 8192 rows; read at once by a dropout, 64 MB of normalised rows
+// lose 2% (49.4 against 48.3 us for both calls), 512 MB gain 1 to 8%.
+constexpr int64_t kPastBytes = int64_t{64} << 20;
+
+// f(the constant that n equals); n is one of them.
+template <int N, int... MORE, typename F>
+auto with_const(int n, F f) {
+  if constexpr (sizeof...(MORE) > 0) {
+    if (n != N) return with_const<MORE...>(n, f);
+  }
+  return f(std::integral_constant<int, N>{});
+}
 
 // Workgroups in one dimension of a grid: it holds fewer than 2^32 work-items
 // (a larger one is cut to its low 32 bits without an error).

@@ -1197,8 +1197,11 @@ int pss_position_bias_backward(const pss_scores_params* params, const pss_positi
   const bool bf16 = params->dtype == PSS_BF16;
   if (!pss::bias_grad_fits(bf16, a, m)) return PSS_ERR_UNSUPPORTED;
   CallScratch scratch;
-  st = scratch.take(pss::bias_grad_workspace_bytes(bf16, a, m), stream);
-  if (st != PSS_OK) return st;
+  const size_t need = pss::bias_grad_workspace_bytes(bf16, a, m);
+  if (need > 0) {
+    st = scratch.take(need, stream);
+    if (st != PSS_OK) return st;
+  }
   const hipError_t e = pss::launch_bias_grad(bf16, a, m, scratch.ptr(), grad_table, stream);
   const hipError_t ef = scratch.done();
   return (e != hipSuccess || ef != hipSuccess) ? PSS_ERR_HIP : PSS_OK;

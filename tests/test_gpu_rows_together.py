@@ -1,0 +1,250 @@
+"""The operators as a sequence layer uses them together: embedding lookup, layer
+norm, attention scores with the position bias, dropout and residual into a
+second norm, all the way back into the shared array; and results in place at
+widths where a row ends inside a vector or a wavefront's span."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pss_oracle as po
+from oracle import rows_oracle as ro
+from paper_2207_10731_amd import pss
+from rows_common import EPS, U, make_drop, make_rows, mask_of, numpy64, rounded, sum_ref, within
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+S, L, H, D, M, Z = 3, 17, 2, 64, 5000, 16  # sequences, tokens, heads, width, shared array, chunk
+N, DH = S * L, D // H
+NUM, FAR, LR = 8, 12, 0.5
+
+
+def _heads(x):
+    return x.reshape(S, L, H, DH).permute(0, 2, 1, 3).contiguous()
+
+
+def _rows(x):
+    return x.permute(0, 2, 1, 3).reshape(N, D).contiguous()
+
+
+def _layer(dev):
+    """Inputs of one training step: token ids, weights, gradients of the outputs."""
+    rng = np.random.default_rng(21)
+    t = lambda *s, shift=0.0, scale=1.0: torch.from_numpy(  # noqa: E731
+        rng.normal(shift, scale, s).astype(np.float32)).to(dev)
+    return dict(ids=rng.integers(0, 300, N), w=t(M), table=t(NUM, H), w1=t(D, shift=1, scale=0.1),
+                b1=t(D, scale=0.1), w2=t(D, shift=1, scale=0.1), b2=t(D, scale=0.1), g_out=t(N, D),
+                g_sum=t(N, D))
+
+
+def _gpu_step(p):
+    hp = pss.make_hash_params(seed=5, num_tables=1, batch=N, num_indices=N)
+    ids = torch.from_numpy(p["ids"]).cuda()
+    offsets = torch.arange(N + 1, device="cuda")
+    drop = make_drop(0.25, 9, 4)
+    buckets = pss.make_position_buckets(NUM, FAR, True)
+    rows = lambda: torch.empty(N, D, device="cuda")  # noqa: E731
+    vec = lambda n: torch.empty(n, device="cuda")  # noqa: E731
+    shared, x0 = p["w"].clone(), rows()
+    pss.pss_forward(shared, M, Z, D, hp, ids, offsets, x0)
+    n1, mean1, rstd1 = rows(), vec(N), vec(N)
+    pss.pss_layer_norm_forward(x0, p["w1"], p["b1"], EPS, n1, mean1, rstd1)
+    q = _heads(n1)
+    scores = torch.matmul(q, q.transpose(-1, -2).contiguous()) / DH**0.5
+    pss.pss_position_bias_forward(p["table"], buckets, scores, scores=scores)
+    prob = torch.softmax(scores, -1)
+    ctx = _rows(torch.matmul(prob, q))
+    out, total, mean2, rstd2 = rows(), rows(), vec(N), vec(N)
+    pss.pss_layer_norm_forward(ctx, p["w2"], p["b2"], EPS, out, mean2, rstd2, residual=x0,
+                               dropout=drop, sum_out=total)
+    # back
+    g_ctx, g_x0, gw2, gb2 = rows(), rows(), vec(D), vec(D)
+    pss.pss_layer_norm_backward(p["g_out"], total, p["w2"], mean2, rstd2, g_ctx, gw2, gb2,
+                                grad_sum=p["g_sum"], dropout=drop, grad_residual=g_x0)
+    gc = _heads(g_ctx)
+    gp = torch.matmul(gc, q.transpose(-1, -2).contiguous())
+    gs = prob * (gp - (gp * prob).sum(-1, keepdim=True))
+    g_table = torch.empty(NUM, H, device="cuda")
+    pss.pss_position_bias_backward(gs, buckets, g_table)
+    gq = torch.matmul(prob.transpose(-1, -2).contiguous(), gc)
+    gq += torch.matmul(gs + gs.transpose(-1, -2), q) / DH**0.5
+    g1, gw1, gb1 = rows(), vec(D), vec(D)
+    # the sum of both gradients of x0, written over the first
+    pss.pss_layer_norm_backward(_rows(gq), x0, p["w1"], mean1, rstd1, g1, gw1, gb1, grad_sum=g_x0)
+    pss.pss_backward_update(shared, None, M, Z, D, hp, ids, offsets, g1, LR)
+    return dict(out=out, total=total, g_table=g_table, gw1=gw1, gb1=gb1, gw2=gw2, gb2=gb2,
+                shared=shared), hp, drop
+
+
+def _reference(p, hp, drop):
+    """The same step in float64 by torch's differentiation on the CPU."""
+    leaf = {k: v.double().cpu().requires_grad_() for k, v in p.items()
+            if k in ("w", "table", "w1", "b1", "w2", "b2")}
+    at = torch.from_numpy(po.element_addresses(M, Z, D, 1, N, hp.a, hp.b, p["ids"],
+                                               np.arange(N + 1)).astype(np.int64)).reshape(N, D)
+    kept, scale = mask_of(drop, N, D)
+
+    def norm(x, w, b):
+        e = x - x.mean(1, keepdim=True)
+        return e / ((e * e).mean(1, keepdim=True) + EPS).sqrt() * w + b
+
+    buckets = torch.from_numpy(ro.bucket_matrix(0, L, L, lambda n: ro.bucket(n, NUM, FAR, True)))
+    x0 = leaf["w"][at]
+    q = _heads(norm(x0, leaf["w1"], leaf["b1"]))
+    scores = q @ q.transpose(-1, -2) / DH**0.5 + leaf["table"][buckets].permute(2, 0, 1)
+    ctx = _rows(torch.softmax(scores, -1) @ q)
+    total = x0 + torch.where(torch.from_numpy(kept), ctx * scale, 0.0)
+    out = norm(total, leaf["w2"], leaf["b2"])
+    ((out * p["g_out"].double().cpu()).sum() + (total * p["g_sum"].double().cpu()).sum()).backward()
+    g = {k: v.grad for k, v in leaf.items()}
+    return dict(out=out.detach(), total=total.detach(), g_table=g["table"], gw1=g["w1"], gb1=g["b1"],
+                gw2=g["w2"], gb2=g["b2"], shared=leaf["w"].detach() - LR * g["w"])
+
+
+def test_training_step_of_a_sequence_layer():
+    """Every result and gradient of the step.  The longest path has two row
+    sums of 64 forward and two back (88 additions each with their trees),
+    products and sums of 17 and 32 terms (about 150) and at most 867 pairs of
+    a bucket or 51 rows: below 1500 roundings; the norms' and the softmax's
+    derivatives (rstd about 1, weights about 1) may double an error each, so
+    that 4 * 1500 u of the largest magnitude bounds it."""
+    p = _layer("cuda")
+    got, hp, drop = _gpu_step(p)
+    want = _reference(p, hp, drop)
+    for k, ref in want.items():
+        ref = ref.numpy()
+        within(got[k], ref, 6000 * U * np.abs(ref).max(), k)
+
+
+def test_step_replayed_from_a_graph():
+    """The operators of the step captured together, with the library's lookup:
+    each replay leaves the bits of the eager step."""
+    p = _layer("cuda")
+    hp = pss.make_hash_params(seed=5, num_tables=1, batch=N, num_indices=N)
+    ids, offsets = torch.from_numpy(p["ids"]).cuda(), torch.arange(N + 1, device="cuda")
+    drop, buckets = make_drop(0.25, 9, 4), pss.make_position_buckets(NUM, FAR, True)
+    x0, out, total, gx = (torch.empty(N, D, device="cuda") for _ in range(4))
+    mean, rstd, gw, gb = (torch.empty(n, device="cuda") for n in (N, N, D, D))
+    scores, gt = torch.randn(S, H, L, L, device="cuda"), torch.empty(NUM, H, device="cuda")
+    biased = torch.empty_like(scores)
+
+    def run():
+        pss.pss_forward(p["w"], M, Z, D, hp, ids, offsets, x0)
+        pss.pss_position_bias_forward(p["table"], buckets, biased, scores=scores)
+        pss.pss_layer_norm_forward(x0, p["w1"], p["b1"], EPS, out, mean, rstd, residual=p["g_sum"],
+                                   dropout=drop, sum_out=total)
+        pss.pss_layer_norm_backward(p["g_out"], total, p["w1"], mean, rstd, gx, gw, gb, dropout=drop)
+        pss.pss_position_bias_backward(biased, buckets, gt)
+
+    results = (x0, out, total, gx, mean, rstd, gw, gb, biased, gt)
+    run()
+    want = [t.clone() for t in results]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for _ in range(3):
+        for t in results:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip(results, want):
+            assert torch.equal(t, w)
+        run()  # eager work between the replays
+
+
+def test_new_token_agrees_with_the_prompt():
+    """The bias of one new token at its place is the prompt's row for it, bit
+    for bit, for every place of a sequence."""
+    m = pss.make_position_buckets(32, 128, False)
+    for K in (70, 517):
+        table = torch.randn(32, 3, device="cuda")
+        scores = torch.randn(1, 3, K, K, device="cuda")
+        prompt = torch.empty_like(scores)
+        pss.pss_position_bias_forward(table, m, prompt, scores=scores)
+        # every query as a sequence of its own, at its own start
+        rows = scores[0].permute(1, 0, 2)[:, :, None, :]
+        starts = torch.arange(K, dtype=torch.int32, device="cuda")
+        token = torch.empty(K, 3, 1, K, device="cuda")
+        pss.pss_position_bias_forward(table, m, token, scores=rows, q_starts=starts)
+        assert torch.equal(token[:, :, 0].permute(1, 0, 2), prompt[0])
+
+
+# Widths whose rows end inside a vector: in the first lane of a span or a
+# wavefront, in another one, in a group of lanes.
+ENDS = [5, 9, 77, 511, 513, 515, 1001, 1025, 2051, 4097, 4101, 9003, 16390]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", ENDS)
+def test_rows_in_place_at_odd_widths(cols, dtype):
+    """Every result over its own input: the same bits as in arrays apart."""
+    rng = np.random.default_rng(cols)
+    rows = 37
+    x, r, dy, up = (make_rows(rng, rows, cols, dtype) for _ in range(4))
+    w, drop = make_rows(rng, 1, cols, F32, 0.3, 1.0)[0], make_drop(0.25)
+    apart = [torch.empty_like(x) for _ in range(5)]
+    mean, rstd, gw, gb = (torch.empty(n, device="cuda") for n in (rows, rows, cols, cols))
+    pss.pss_dropout(x, drop, apart[0], residual=r)
+    kept, scale = mask_of(drop, rows, cols)
+    s, err = sum_ref(numpy64(x), numpy64(r), kept, scale)
+    within(apart[0], s, rounded(s, err, dtype), "dropout")
+    pss.pss_layer_norm_forward(x, w, None, EPS, apart[1], mean, rstd, residual=r, dropout=drop,
+                               sum_out=apart[2])
+    pss.pss_layer_norm_backward(dy, apart[2], w, mean, rstd, apart[3], gw, gb, grad_sum=up,
+                                dropout=drop, grad_residual=apart[4])
+    for over in (0, 1):
+        a = (x.clone(), r.clone())
+        pss.pss_dropout(a[0], drop, a[over], residual=a[1])
+        assert torch.equal(a[over], apart[0])
+        a = (x.clone(), r.clone())
+        pss.pss_layer_norm_forward(a[0], w, None, EPS, a[over], residual=a[1], dropout=drop,
+                                   sum_out=a[1 - over])
+        assert torch.equal(a[over], apart[1]) and torch.equal(a[1 - over], apart[2])
+        a = [dy.clone(), up.clone(), apart[2].clone()]
+        g = [torch.empty_like(gw), torch.empty_like(gb)]
+        pss.pss_layer_norm_backward(a[0], a[2], w, mean, rstd, a[2 * over], g[0], g[1],
+                                    grad_sum=a[1], dropout=drop, grad_residual=a[1])
+        assert torch.equal(a[2 * over], apart[3]) and torch.equal(a[1], apart[4])
+        assert torch.equal(g[0], gw) and torch.equal(g[1], gb)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("Q,K", [(1, 5), (3, 515), (9, 3), (20, 21), (33, 65), (20, 257), (17, 513), (9, 515),
+                                 (40, 1003), (16, 2049), (8, 4099)])
+def test_scores_in_place_at_odd_lengths(Q, K, dtype):
+    m = pss.make_position_buckets(32, 128, True)
+    B, H_ = 5, 3
+    table = torch.randn(32, H_, device="cuda").to(dtype)
+    x = torch.randn(B, H_, Q, K, device="cuda").to(dtype)
+    starts = torch.arange(B, dtype=torch.int32, device="cuda") * 7
+    out = torch.empty_like(x)
+    pss.pss_position_bias_forward(table, m, out, scores=x, q_starts=starts)
+    buckets = np.stack([ro.bucket_matrix(7 * b, Q, K, lambda n: ro.bucket(n, 32, 128, True))
+                        for b in range(B)])
+    ref = ro.position_bias(numpy64(table), buckets, numpy64(x))
+    within(out, ref, rounded(ref, U * np.abs(ref), dtype), "apart")
+    pss.pss_position_bias_forward(table, m, x, scores=x, q_starts=starts)
+    assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_of_overlapping_and_repeated_input_rows(dtype):
+    """Inputs whose rows share elements: a window one element further a row,
+    and one row for all."""
+    rng = np.random.default_rng(2)
+    base = make_rows(rng, 1, 700, dtype)[0]
+    for view in (base.as_strided((50, 203), (1, 1)), base[:203].expand(50, 203)):
+        out = torch.empty(50, 203, dtype=dtype, device="cuda")
+        mean, rstd = (torch.empty(50, device="cuda") for _ in range(2))
+        pss.pss_layer_norm_forward(view, None, None, EPS, out, mean, rstd)
+        same = torch.empty_like(out)
+        pss.pss_layer_norm_forward(view.contiguous(), None, None, EPS, same)
+        assert torch.equal(out, same)
+        gx, gs = torch.empty_like(out), torch.empty_like(out)
+        g = [torch.empty(203, device="cuda") for _ in range(4)]
+        pss.pss_layer_norm_backward(view, view, None, mean, rstd, gx, g[0], g[1])
+        pss.pss_layer_norm_backward(view.contiguous(), view.contiguous(), None, mean, rstd, gs, g[2],
+                                    g[3])
+        assert torch.equal(gx, gs) and torch.equal(g[0], g[2]) and torch.equal(g[1], g[3])

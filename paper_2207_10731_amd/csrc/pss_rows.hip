@@ -40,7 +40,10 @@ static hipError_t by_row_type(bool bf16, int64_t cols, F f) {
 }
 
 // ---------------------------------------------------------------------------
-// out = residual + D(x): a span of a row to a group of G lanes.
+// out = residual + D(x): a span of a row to a group of G lanes.  Ten rounds of the
+// generator make the numbers of 8 elements, about 60 instructions that the loads
+// hide: bound by memory, 2 row arrays or 3.  32768 x 4096 bfloat16 with residual:
+// 121 us, 6.6 TB/s; 16384 x 3328 float32: 68 us, 6.4 TB/s (a large copy: 6.2).
 // ---------------------------------------------------------------------------
 template <typename T, int G, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, const RowsIn residual,
@@ -123,7 +126,9 @@ hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, co
 // registers: up to 1024 columns a group of lanes takes a row, beyond that a block
 // of as many wavefronts as the row fills.  Groups and blocks walk over rows, with
 // the row after the present one already requested and the weights in
-// registers.  Bound by memory: 2 to 4 row arrays read or written.
+// registers.  Bound by memory: 2 to 4 row arrays read or written.  425984 x 128
+// float32: 76 us, 5.7 TB/s; 16384 x 4096 bfloat16 with residual and dropout:
+// 100 us, 5.4 TB/s (a block a row that reads it three times: 909 and 175 us).
 // ---------------------------------------------------------------------------
 
 // What a row needs of one span.
@@ -339,7 +344,8 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
 
 // Wider rows: a block a row, which it reads three times (sum, squares about the
 // mean, result), the last two from L2.  Nothing is stored before the last pass,
-// where every element is read by the lane that then stores its results.
+// where every element is read by the lane that then stores its results.  1024 x
+// 30000 float32: 92 us, 2.7 TB/s of the two arrays.
 template <typename T, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2 * kRowWaves];
@@ -470,7 +476,9 @@ hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream
 // gradients in registers and writes them to its own row of parts
 // ([blocks][2][cols]); sum_parts_kernel adds the blocks' rows in order.  A few
 // rows are one block's, which writes the gradients themselves.
-// Bound by memory: 3 to 5 row arrays.
+// Bound by memory: 3 to 5 row arrays.  16384 x 4096 bfloat16 with residual and
+// dropout: 125 us, 5.4 TB/s; 53248 x 128 float32: 22 us (19 and 4 for the parts'
+// sum), 3.8 TB/s.  (Stored past the caches: 3 to 16% slower.)
 // ---------------------------------------------------------------------------
 
 // Where a block's sums go: element c of block k's at weight[k * 2 * cols + c] (of

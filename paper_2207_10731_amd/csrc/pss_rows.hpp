@@ -441,10 +441,11 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
 
-// Results of more than this are stored past the caches where that is faster: alone,
-// bias of 2 x 16 x 2048 x 2048 bfloat16 88 against 94 us, norm of 16384 x 4096
-// 50 against 54 with 8192 rows; read at once by a dropout, 64 MB of normalised rows
-// lose 2% (49.4 against 48.3 us for both calls), 512 MB gain 1 to 8%.
+// Results of more than this are stored past the caches.  Alone such a call gains 3 to
+// 15% (bias of 2 x 16 x 2048 x 2048 bfloat16 88 against 94 us, norm of 262144 x 128
+// float32 47 against 50); where the next call reads its results, the two together
+// lose 2% at 64 MB (norm, then dropout: 49.4 against 48.3 us) and gain 1 to 8% at
+// 512 MB; below 64 MB a program has the results in the caches next.
 constexpr int64_t kPastBytes = int64_t{64} << 20;
 
 // f(the constant that n equals); n is one of them.

@@ -433,7 +433,8 @@ int pss_dropout(const pss_rows_params* params, const pss_dropout_params* dropout
  * mean, rstd  device float32[R], or NULL: kept for the backward pass
  * weight, bias  device, C elements of params->weight_dtype, or NULL
  * eps      > 0, finite
- * s is normalised as float32, before it is rounded for sum_out. */
+ * s is normalised as float32, before it is rounded for sum_out.  (Squares are
+ * float32 too: a row that reaches 1e19 from its mean overflows to rstd = 0.) */
 int pss_layer_norm_forward(const pss_rows_params* params, const pss_dropout_params* dropout,
                            const void* x, int64_t x_stride, const void* residual,
                            int64_t residual_stride, const void* weight, const void* bias, float eps,

@@ -424,14 +424,17 @@ static RowForm norm_form(bool bf16, int64_t cols) {
   if (two) return {static_cast<int>(w2) * kWave, 2, kHeld};
   return {static_cast<int>(w1) * kWave, 1, static_cast<int>(held)};
 }
-// Blocks that walk rows: what the CUs hold, with as many rows to each (a second
-// round of blocks would take as long as the first).
+// Blocks that walk rows: what the CUs hold, with as many rows to each (a last
+// round of a few rows takes as long as the others: 16000 x 2500 float32 55 against
+// 57 us).  Narrow rows, many to a block, fill the CUs instead (backward of 53248 x
+// 128 float32 20.9 against 21.6 us).
 static uint32_t row_blocks(const RowForm& f, int64_t rows) {
   const bool group = f.lanes <= kWave;
   const int64_t per_block = group ? kRowThreads / f.lanes : 1;
   const int64_t want = (rows + per_block - 1) / per_block;
   const int64_t held = int64_t{256} * (f.waves * kWave / (group ? kRowThreads : f.lanes));
   const int64_t rounds = (want + held - 1) / held;
+  if (f.lanes < kWave && rounds > 2) return static_cast<uint32_t>(held);
   return static_cast<uint32_t>((want + rounds - 1) / rounds);
 }
 

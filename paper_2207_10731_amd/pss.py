@@ -291,7 +291,7 @@ def _weight_dtype(shared):
 # raise, or accept, as they always have.
 _WEIGHTS = {PSS_F32: torch.float32, PSS_BF16: torch.bfloat16}
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _fits(t, dtype, n, dev):
@@ -593,26 +593,28 @@ def _rows_of(name, t, shape, dtype, dev, out):
     return t.data_ptr(), stride
 
 
-def _first_device(name, t):
-    """GPU of the tensor that sets the call's shape: the current one."""
-    dev = t.get_device()
-    if dev < 0:
+def _not_current(name, t):
+    """Raises: the tensor that sets the call's shape is not on the current GPU."""
+    if t.get_device() < 0:
         raise ValueError(f"{name} must be a GPU tensor")
-    if dev != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
-        raise ValueError(f"tensor on {t.device}, current device is "
-                         f"cuda:{torch.cuda.current_device()}")
-    return dev
+    raise ValueError(f"tensor on {t.device}, current device is "
+                     f"cuda:{torch.cuda.current_device()}")
 
 
 def _first_rows(name, t):
-    """(PSS type, shape, type, GPU) of the row argument that sets the call's shape."""
-    dtype, shape = t.dtype, t.shape
+    """(PSS type, shape, type, GPU, address, stride) of the row argument that sets
+    the call's shape."""
+    dtype, shape, dev = t.dtype, t.shape, t.get_device()
     kind = _ROW_DTYPES.get(dtype)
     if kind is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}")
     if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{name} must be [rows][cols] with cols > 0, got {tuple(shape)}")
-    return kind, shape, dtype, _first_device(name, t)
+    if dev < 0 or dev != _current_device():
+        _not_current(name, t)
+    if t.is_contiguous():
+        return kind, shape, dtype, dev, t.data_ptr(), shape[1]
+    return (kind, shape, dtype, dev) + _rows_of(name, t, shape, dtype, dev, False)
 
 
 def _vector(name, t, dtype, n, dev):
@@ -629,8 +631,6 @@ def _vector(name, t, dtype, n, dev):
 
 
 def _drop_arg(dropout, dev):
-    if dropout is None:
-        return None
     address = getattr(dropout, "address", None)
     if address is None:  # a block that the caller filled
         return ctypes.byref(dropout)
@@ -643,10 +643,9 @@ def pss_dropout(x, dropout, out, residual=None, stream=None):
     """out = residual + D(x); the gradient of x is the same call on that of
     out.  x, out, residual: [rows][cols]; ``dropout``: make_dropout_params."""
     lib = load_library()
-    kind, shape, dtype, dev = _first_rows("x", x)
+    kind, shape, dtype, dev, xp, xs = _first_rows("x", x)
     if dropout is None:
         raise ValueError("dropout is missing: make_dropout_params")
-    xp, xs = _row_arg("x", x, shape, dtype, dev)
     op, os_ = _row_arg("out", out, shape, dtype, dev, True)
     rp, rs = ((None, 0) if residual is None else
               _row_arg("residual", residual, shape, dtype, dev))
@@ -674,9 +673,8 @@ def pss_layer_norm_forward(x, weight, bias, eps, out, mean=None, rstd=None, resi
     """out = layer norm of s = residual + D(x), row by row; sum_out receives s,
     mean and rstd (float32 [rows]) what the backward pass needs."""
     lib = load_library()
-    kind, shape, dtype, dev = _first_rows("x", x)
+    kind, shape, dtype, dev, xp, xs = _first_rows("x", x)
     rows, cols = shape
-    xp, xs = _row_arg("x", x, shape, dtype, dev)
     op, os_ = _row_arg("out", out, shape, dtype, dev, True)
     rp, rs = ((None, 0) if residual is None else
               _row_arg("residual", residual, shape, dtype, dev))
@@ -684,7 +682,8 @@ def pss_layer_norm_forward(x, weight, bias, eps, out, mean=None, rstd=None, resi
               _row_arg("sum_out", sum_out, shape, dtype, dev, True))
     wkind, wp, bp = _norm_weights(weight, bias, cols, dev)
     _check(lib.pss_layer_norm_forward(
-        _rows_params(rows, cols, kind, wkind), _drop_arg(dropout, dev), xp, xs,
+        _rows_params(rows, cols, kind, wkind),
+        None if dropout is None else _drop_arg(dropout, dev), xp, xs,
         rp, rs, wp, bp, eps, op, os_, sp, ss, _vector("mean", mean, torch.float32, rows, dev),
         _vector("rstd", rstd, torch.float32, rows, dev), _raw_stream(stream, dev)),
         "pss_layer_norm_forward")
@@ -699,9 +698,8 @@ def pss_layer_norm_backward(grad_out, s, weight, mean, rstd, grad_x, grad_weight
     not wanted.  s: sum_out (or x); grad_sum: the gradient that reaches sum_out
     from elsewhere."""
     lib = load_library()
-    kind, shape, dtype, dev = _first_rows("grad_out", grad_out)
+    kind, shape, dtype, dev, gp, gs = _first_rows("grad_out", grad_out)
     rows, cols = shape
-    gp, gs = _row_arg("grad_out", grad_out, shape, dtype, dev)
     sp, ss = _row_arg("s", s, shape, dtype, dev)
     up, us = ((None, 0) if grad_sum is None else
               _row_arg("grad_sum", grad_sum, shape, dtype, dev))
@@ -713,7 +711,8 @@ def pss_layer_norm_backward(grad_out, s, weight, mean, rstd, grad_x, grad_weight
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward call are needed")
     _check(lib.pss_layer_norm_backward(
-        _rows_params(rows, cols, kind, wkind), _drop_arg(dropout, dev), gp, gs,
+        _rows_params(rows, cols, kind, wkind),
+        None if dropout is None else _drop_arg(dropout, dev), gp, gs,
         sp, ss, wp, _vector("mean", mean, torch.float32, rows, dev),
         _vector("rstd", rstd, torch.float32, rows, dev), up, us, xp, xs, rp, rs,
         _vector("grad_weight", grad_weight, torch.float32, cols, dev),
@@ -755,13 +754,15 @@ def _scores_of(name, t, shape, dtype, dev):
 
 
 def _bias_sizes(name, t):
-    dtype, shape = t.dtype, t.shape
+    dtype, shape, dev = t.dtype, t.shape, t.get_device()
     kind = _ROW_DTYPES.get(dtype)
     if kind is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}")
     if len(shape) != 4:
         raise ValueError(f"{name} must be [B][H][Q][K], got {tuple(shape)}")
-    return kind, shape, dtype, _first_device(name, t)
+    if dev < 0 or dev != _current_device():
+        _not_current(name, t)
+    return kind, shape, dtype, dev
 
 
 def _table_of(name, table, buckets, heads, dev):

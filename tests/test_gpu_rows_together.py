@@ -171,6 +171,22 @@ def test_new_token_agrees_with_the_prompt():
         assert torch.equal(token[:, :, 0].permute(1, 0, 2), prompt[0])
 
 
+@pytest.mark.parametrize("Q,K,B", [(2, 300, 3), (30, 50, 2), (40, 600, 1)])
+def test_bias_of_own_borders(Q, K, B):
+    """Borders that a program fills itself: repeated ones, a first bucket of
+    several, one bucket alone; keys on both sides of the queries."""
+    for num, both, borders in ((5, 0, [0, 0, 3, 3, 9]), (8, 1, [0, 0, 3, 40]), (1, 0, [0]), (2, 1, [0]),
+                               (6, 1, [0, 0, 0]), (4, 0, [0, 1, 1, 2000])):
+        m = pss.pss_position_buckets(num, both)
+        m.borders[:len(borders)] = borders
+        buckets = ro.bucket_matrix(10, Q, K, lambda n: int(pss.pss_position_buckets_host(m, [n])[0]))
+        table = torch.randn(num, 3, device="cuda")
+        out = torch.empty(B, 3, Q, K, device="cuda")
+        pss.pss_position_bias_forward(table, m, out, q_start=10)
+        ref = ro.position_bias(numpy64(table), np.repeat(buckets[None], B, 0))
+        assert np.array_equal(numpy64(out), ref), (num, both, borders)
+
+
 # Widths whose rows end inside a vector: in the first lane of a span or a
 # wavefront, in another one, in a group of lanes.
 ENDS = [5, 9, 77, 511, 513, 515, 1001, 1025, 2051, 4097, 4101, 9003, 16390]

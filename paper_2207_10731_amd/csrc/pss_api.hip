@@ -710,6 +710,7 @@ int check_map(const pss_position_buckets* m, pss::BucketMap* out) {
     if (i > 0 && m->borders[i] < m->borders[i - 1]) return PSS_ERR_INVALID_ARG;
     out->borders[i] = m->borders[i];
   }
+  out->far = pss::far_buckets(*out);
   return PSS_OK;
 }
 

@@ -7,6 +7,7 @@ namespace pss {
 constexpr int kBiasThreads = 256;
 constexpr int kBiasWaves = kBiasThreads / kWave;
 constexpr int kMaxStart = 1 << 29;  // of q_starts
+constexpr int kMaxNear = 1024;      // last border that lists and windows of distances hold
 
 // Position of query 0 of batch b.  Positions stay below 3 * 2^29 and keys
 // below 2^30: differences fit 32 bits.
@@ -28,33 +29,21 @@ __device__ __forceinline__ int key_rest(int64_t K) {
   return static_cast<int>(K) & (kVec<T> - 1);
 }
 
-// Buckets of the differences key - query that need no search: beyond the last
-// border, and ahead of the query on a single side.
-struct FarBuckets {
-  int behind, ahead;        // of differences <= -near, >= from
-  int32_t near, from;
-};
-__device__ __forceinline__ FarBuckets far_buckets(const BucketMap& map) {
-  FarBuckets f;
-  f.near = map.borders[map.side - 1];
-  f.behind = map.side - 1;
-  f.from = map.both ? (f.near > 1 ? f.near : 1) : 0;
-  f.ahead = map.num - 1;
-  if (!map.both) {  // the last of the buckets from distance 0 on
-    f.ahead = 0;
-    while (f.ahead + 1 < map.side && map.borders[f.ahead + 1] <= 0) ++f.ahead;
-  }
-  return f;
-}
-
 // ---------------------------------------------------------------------------
 // Forward, few queries (new tokens): 16 bytes of keys a lane.  Buckets are
 // ranges of distances: keys beyond the last border (nearly all of a long cache)
-// need no search, and keys whose ends share a bucket two, not one each.  A
-// wavefront copies the borders to LDS only if it has others.  16 x 32 x 1 x 32768
-// bfloat16: 20 us, 3.4 TB/s; a small call is bound by its launch.
+// need no search.  A wavefront that has others copies the borders to LDS and, up to
+// distances of 1024, makes a list of buckets there, a search to each distance and
+// not to each key; farther, keys whose ends share a bucket need two searches.
+// 64 x 16 x 1 x 4096 bfloat16: 7.1 us a call (a search to each key near the query
+// 9.9), 16 x 32 x 1 x 32768: 14.6 us, 4.6 TB/s (19.7); a small call is bound by its
+// launch.
 // ---------------------------------------------------------------------------
-template <typename T, bool ENDS, bool PAST>
+constexpr int kRowPieces = 4;
+
+// WIDE: 64 lanes or more to a row, so that a wavefront has one.  A lane takes U pieces
+// of keys, tx apart.
+template <typename T, bool ENDS, bool PAST, bool WIDE, int U>
 __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a,
                                                                 const BucketMap map, const int tx,
                                                                 const uint32_t k_tiles,
@@ -62,54 +51,89 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
   constexpr int V = kVec<T>;
   constexpr End kEnd = ENDS ? End::kPieces : End::kWhole;
   __shared__ int32_t all_borders[kBiasWaves][kMaxBuckets];
+  __shared__ uint8_t all_lists[kBiasWaves][kMaxNear];
   const int rest = key_rest<T>(a.K);
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
-  const int64_t k = (static_cast<int64_t>(blockIdx.x % k_tiles) * tx + x) * V;
-  const uint32_t row = tile_of(per, k_tiles) * (kBiasThreads / tx) + y;
-  const bool mine = k < a.K && row < static_cast<uint32_t>(a.B * a.H * a.Q);
+  const uint32_t kt = blockIdx.x % k_tiles;
+  uint32_t row = tile_of(per, k_tiles) * (kBiasThreads / tx) + y;
+  if (WIDE) row = __builtin_amdgcn_readfirstlane(row);
+  const bool any = row < static_cast<uint32_t>(a.B * a.H * a.Q);
+  if (WIDE && !any) return;
   const uint32_t bh = row / static_cast<uint32_t>(a.Q), q = row - bh * static_cast<uint32_t>(a.Q);
   const uint32_t b = bh / static_cast<uint32_t>(a.H), h = bh - b * static_cast<uint32_t>(a.H);
-  const int len = mine ? keys_left(k, a.K) : 0;
-  float v[V];
-  typename Vec<T>::type raw;
-  if (a.in != nullptr)
-    raw = load_vec<kEnd>(static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
-                             q * a.in_stride[2] + k, len, rest);
-  const FarBuckets far = far_buckets(map);
-  const int32_t rel = mine ? static_cast<int32_t>(k) - first_position(a, b) - static_cast<int32_t>(q)
-                           : far.from;
-  const bool is_behind = rel + V - 1 <= -far.near, is_far = is_behind || rel >= far.from;
-  int j0 = is_behind ? far.behind : far.ahead;
-  bool one = true;
+  const int64_t k0 = static_cast<int64_t>(kt) * U * tx * V;  // the tile's
+  const T* in = static_cast<const T*>(a.in) + b * a.in_stride[0] + h * a.in_stride[1] +
+                q * a.in_stride[2] + k0;
+  T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] + q * a.out_stride[2] + k0;
+  typename Vec<T>::type raw[U];
+  int len[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    len[i] = any ? keys_left(k0 + (i * tx + x) * V, a.K) : 0;
+    if (a.in != nullptr) raw[i] = load_vec<kEnd>(in + (i * tx + x) * V, len[i], rest);
+  }
+  const FarBuckets far = map.far;
+  const int32_t pos = any ? first_position(a, b) + static_cast<int32_t>(q) : 0;
+  const float t_behind = any ? table_entry(a, static_cast<int64_t>(far.behind) * a.H + h) : 0.f;
+  const float t_ahead = any ? table_entry(a, static_cast<int64_t>(far.ahead) * a.H + h) : 0.f;
   int32_t* borders = all_borders[threadIdx.x >> 6];
-  if (__any(!is_far)) {
-    for (int i = threadIdx.x & (kWave - 1); i < map.side; i += kWave) borders[i] = map.borders[i];
-    wave_lds_fence();
-    if (!is_far) {
-      j0 = bucket_of(rel, borders, map.side, map.both);
-      // behind the query buckets fall with the key, ahead of it they rise: equal
-      // ends on one side of it hold all between
-      one = j0 == bucket_of(rel + V - 1, borders, map.side, map.both) &&
-            (rel >= 0 || rel + V - 1 <= 0);
+  uint8_t* list = all_lists[threadIdx.x >> 6];
+  const bool listed = far.near <= kMaxNear;
+  bool copied = false;
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int32_t rel = static_cast<int32_t>(k0) + (i * tx + x) * V - pos;
+    const bool is_behind = rel + V - 1 <= -far.near;
+    const bool is_near = len[i] > 0 && !is_behind && rel < far.from;
+    float v[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) v[u] = is_behind ? t_behind : t_ahead;
+    if (__any(is_near)) {
+      if (!copied) {
+        for (int j = threadIdx.x & (kWave - 1); j < map.side; j += kWave) borders[j] = map.borders[j];
+        wave_lds_fence();
+        if (listed) {
+          for (int n = threadIdx.x & (kWave - 1); n < far.near; n += kWave)
+            list[n] = static_cast<uint8_t>(bucket_of(-n, borders, map.side, map.both));
+          wave_lds_fence();
+        }
+        copied = true;
+      }
+      if (is_near && listed) {
+        int j[V];
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+          const int32_t r = rel + u, n = r < 0 ? -r : r;
+          const bool in_list = n < far.near && r < far.from;
+          j[u] = list[in_list ? n : 0] + (r > 0 ? map.side : 0);
+          if (!in_list) j[u] = r < far.from ? far.behind : far.ahead;
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u) v[u] = table_entry(a, static_cast<int64_t>(j[u]) * a.H + h);
+      } else if (is_near) {
+        const int j0 = bucket_of(rel, borders, map.side, map.both);
+        // behind the query buckets fall with the key, ahead of it they rise: equal
+        // ends on one side of it hold all between
+        const bool one = j0 == bucket_of(rel + V - 1, borders, map.side, map.both) &&
+                         (rel >= 0 || rel + V - 1 <= 0);
+        v[0] = table_entry(a, static_cast<int64_t>(j0) * a.H + h);
+#pragma unroll
+        for (int u = 1; u < V; ++u) v[u] = v[0];
+        if (!one) {
+#pragma unroll
+          for (int u = 1; u < V; ++u)
+            v[u] = table_entry(
+                a, static_cast<int64_t>(bucket_of(rel + u, borders, map.side, map.both)) * a.H + h);
+        }
+      }
     }
-  }
-  if (!mine) return;
-  if (one) {
-    const float t = table_entry(a, j0 * a.H + h);
+    if (a.in != nullptr) {
+      raw[i] = settle<kEnd>(raw[i], len[i], rest);
 #pragma unroll
-    for (int u = 0; u < V; ++u) v[u] = t;
-  } else {
-#pragma unroll
-    for (int u = 0; u < V; ++u)
-      v[u] = table_entry(a, bucket_of(rel + u, borders, map.side, map.both) * a.H + h);
+      for (int u = 0; u < V; ++u) v[u] += widen(raw[i][u]);
+    }
+    store_vec<ENDS, PAST>(out + (i * tx + x) * V, v, len[i]);
   }
-  if (a.in != nullptr) {
-    raw = settle<kEnd>(raw, len, rest);
-#pragma unroll
-    for (int u = 0; u < V; ++u) v[u] += widen(raw[u]);
-  }
-  store_vec<ENDS, PAST>(static_cast<T*>(a.out) + b * a.out_stride[0] + h * a.out_stride[1] +
-                            q * a.out_stride[2] + k, v, len);
 }
 
 // ---------------------------------------------------------------------------
@@ -173,7 +197,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_tile_kernel(const BiasArgs 
   const int size = kKeys + rows;  // of a window, with one more than it needs
   // difference of its first entry: the tile's first key, its last query
   const int32_t rel0 = static_cast<int32_t>(k0 - q0 - (rows - 1));
-  const FarBuckets far = far_buckets(map);
+  const FarBuckets far = map.far;
   const auto bucket = [&](int32_t rel) {
     if (rel <= -far.near) return far.behind;
     return rel >= far.from ? far.ahead : bucket_of(rel, borders, map.side, map.both);
@@ -244,18 +268,37 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
   const bool past = bh * a.Q * a.K * static_cast<int64_t>(sizeof(T)) > kPastBytes &&
                     (sizeof(T) == 4 || tx >= kWave || a.K % 32 == 0);
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
-    const int64_t row_tiles = (bh * a.Q + ty - 1) / ty;
-    const TileGrid tg = tile_grid(row_tiles, k_tiles);
+    // several pieces a lane, as long as they leave 2 blocks to a CU (16 x 32 x 1 x 32768
+    // float32 26 against 30 us); bfloat16 rows that end inside a piece one (4100 keys
+    // of 64 x 16: 11.2 against 15.0 us)
+    int pieces = 1, lanes = tx;
+    for (int n = kRowPieces; n > 1 && pieces == 1; n /= 2) {
+      const int64_t step = n * kVec<T>;  // keys of a lane
+      if (a.K < step * kWave || (sizeof(T) == 2 && a.K % kVec<T> != 0)) continue;
+      const int t = key_lanes(a.K, static_cast<int>(step), kWave, kBiasThreads);
+      const int64_t rows = kBiasThreads / t, across = step * t;
+      if ((bh * a.Q + rows - 1) / rows * ((a.K + across - 1) / across) < 512) continue;
+      pieces = n;
+      lanes = t;
+    }
+    const int64_t rows = kBiasThreads / lanes, across = static_cast<int64_t>(lanes) * pieces * kVec<T>;
+    const int64_t tiles = (a.K + across - 1) / across;
+    const TileGrid tg = tile_grid((bh * a.Q + rows - 1) / rows, tiles);
     if (!tg.fits) return hipErrorInvalidConfiguration;
     const auto launch = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, tx,
-                         static_cast<uint32_t>(k_tiles), tg.per);
+      hipLaunchKernelGGL(kernel, tg.grid, block, 0, stream, a, map, lanes,
+                         static_cast<uint32_t>(tiles), tg.per);
       return hipGetLastError();
     };
-    return by_store(past, [&](auto to) {
-      return a.K % kVec<T> ? launch(bias_row_kernel<T, true, to.value>)
-                           : launch(bias_row_kernel<T, false, to.value>);
-    });
+    const auto with_ends = [&](auto ends) {
+      return by_store(past, [&](auto to) {
+        if (lanes < kWave) return launch(bias_row_kernel<T, ends.value, to.value, false, 1>);
+        return with_const<1, 2, kRowPieces>(pieces, [&](auto n) {
+          return launch(bias_row_kernel<T, ends.value, to.value, true, n.value>);
+        });
+      });
+    };
+    return a.K % kVec<T> ? with_ends(std::true_type{}) : with_ends(std::false_type{});
   }
   BiasTile tl;
   tl.pairs = 1;
@@ -312,7 +355,6 @@ hipError_t launch_bias(bool bf16, const BiasArgs& a, const BucketMap& map, hipSt
 // 2048 bfloat16 93 us, 5.8 TB/s (5 for the blocks' sums); small calls by their
 // launches.
 // ---------------------------------------------------------------------------
-constexpr int kMaxNear = 1024;        // last border of this form
 // Units that one block takes alone (1 x 16 x 128 x 128 bfloat16: 7.6 against 9.7 us a
 // call; twice as many, 16 x 8 x 1 x 512: 11.6 against 9.6).
 constexpr int kAloneUnits = 2 * kBiasWaves;
@@ -392,16 +434,16 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
   extern __shared__ float windows[];  // [wavefront][window]
   __shared__ int32_t borders[kMaxBuckets];
   __shared__ float far[2][kBiasWaves];
-  for (int i = threadIdx.x; i < kBiasWaves * window; i += kBiasThreads) windows[i] = 0.f;
-  for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];
-  __syncthreads();
-  const int near = borders[map.side - 1];
-  const int ahead = map.both ? (near > 1 ? near : 1) : 0;  // differences from here on are far
+  for (int i = threadIdx.x; i < map.side; i += kBiasThreads) borders[i] = map.borders[i];  // the end's
+  const int near = map.far.near;
+  const int ahead = map.far.from;          // differences from here on are far
   const int zero = near + kNearPad;                        // window[zero]: difference 0
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int x = lane % TX, group = lane / TX;
   float* mine = windows + wave * window;
+  for (int i = lane; i < window; i += kWave) mine[i] = 0.f;
+  wave_lds_fence();
   const uint32_t h = blockIdx.y;
   // the wavefront's units: rows of steps, each k_steps long
   const int64_t waves = static_cast<int64_t>(gridDim.x) * kBiasWaves;
@@ -476,8 +518,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
     windows[i] = v;
   }
   __syncthreads();
-  const int behind_bucket = map.side - 1;
-  const int ahead_bucket = map.both ? map.num - 1 : bucket_of(0, borders, map.side, false);
+  const int behind_bucket = map.far.behind, ahead_bucket = map.far.ahead;
   for (int j = wave; j < map.num; j += kBiasWaves) {
     int32_t lo, hi;
     bucket_range(j, borders, map, &lo, &hi);

@@ -61,10 +61,29 @@ struct NormGradArgs {
 
 // Position buckets: `num` in all, one side's `side` borders.
 constexpr int kMaxBuckets = 256;
+// Those of the differences key - query that need no search: beyond the last border,
+// and ahead of the query on a single side.
+struct FarBuckets {
+  int32_t behind = 0, ahead = 0;  // of differences <= -near, >= from
+  int32_t near = 0, from = 0;
+};
 struct BucketMap {
   int32_t num = 0, side = 0, both = 0;
+  FarBuckets far;  // ahead of the borders: a kernel needs them before those
   int32_t borders[kMaxBuckets];
 };
+inline FarBuckets far_buckets(const BucketMap& map) {
+  FarBuckets f;
+  f.near = map.borders[map.side - 1];
+  f.behind = map.side - 1;
+  f.from = map.both ? (f.near > 1 ? f.near : 1) : 0;
+  f.ahead = map.num - 1;
+  if (!map.both) {  // the last of the buckets from distance 0 on
+    f.ahead = 0;
+    while (f.ahead + 1 < map.side && map.borders[f.ahead + 1] <= 0) ++f.ahead;
+  }
+  return f;
+}
 
 struct BiasArgs {
   int64_t B = 0, H = 0, Q = 0, K = 0;

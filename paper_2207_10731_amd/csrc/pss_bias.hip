@@ -269,12 +269,11 @@ static hipError_t launch_bias_t(const BiasArgs& a, const BucketMap& map, hipStre
                     (sizeof(T) == 4 || tx >= kWave || a.K % 32 == 0);
   if (a.Q < kStep && bh * a.Q <= INT32_MAX) {
     // several pieces a lane, as long as they leave 2 blocks to a CU (16 x 32 x 1 x 32768
-    // float32 26 against 30 us); bfloat16 rows that end inside a piece one (4100 keys
-    // of 64 x 16: 11.2 against 15.0 us)
+    // float32 26 against 30 us)
     int pieces = 1, lanes = tx;
     for (int n = kRowPieces; n > 1 && pieces == 1; n /= 2) {
       const int64_t step = n * kVec<T>;  // keys of a lane
-      if (a.K < step * kWave || (sizeof(T) == 2 && a.K % kVec<T> != 0)) continue;
+      if (a.K < step * kWave) continue;
       const int t = key_lanes(a.K, static_cast<int>(step), kWave, kBiasThreads);
       const int64_t rows = kBiasThreads / t, across = step * t;
       if ((bh * a.Q + rows - 1) / rows * ((a.K + across - 1) / across) < 512) continue;

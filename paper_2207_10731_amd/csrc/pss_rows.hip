@@ -127,7 +127,7 @@ hipError_t launch_dropout(bool bf16, const RowsIn& x, const RowsIn& residual, co
 // of as many wavefronts as the row fills.  Groups and blocks walk over rows, with
 // the row after the present one already requested and the weights in
 // registers.  Bound by memory: 2 to 4 row arrays read or written.  425984 x 128
-// float32: 76 us, 5.7 TB/s; 16384 x 4096 bfloat16 with residual and dropout:
+// float32: 71 us, 6.2 TB/s; 16384 x 4096 bfloat16 with residual and dropout:
 // 100 us, 5.4 TB/s (a block a row that reads it three times: 909 and 175 us).
 // ---------------------------------------------------------------------------
 
@@ -438,33 +438,51 @@ static uint32_t row_blocks(const RowForm& f, int64_t rows) {
   return static_cast<uint32_t>((want + rounds - 1) / rounds);
 }
 
+// The forward of rows of whole vectors: groups take a row and are done, or two
+// without a residual, rather than walk over the array, where the results go past the
+// caches and for bfloat16 with a residual (262144 x 128 with residual and dropout:
+// float32 90 against 96 us, bfloat16 50 against 53; without, float32 45 against 47; but
+// 65536 x 256 float32, results through the caches, 52 against 50).  Half-empty bfloat16
+// spans (40000 x 520) lose by it, and so do rows that end inside a vector.
+template <typename T, bool ENDS, bool PAST>
+static uint32_t norm_blocks(const RowForm& f, const NormArgs& a) {
+  const uint32_t walking = row_blocks(f, a.rows);
+  const bool gains = PAST || (sizeof(T) == 2 && a.residual.p != nullptr);
+  if (ENDS || !gains || f.lanes > kWave || (sizeof(T) == 2 && f.spans == 2)) return walking;
+  const int64_t each = (kRowThreads / f.lanes) * (a.residual.p != nullptr ? 1 : 2);
+  const int64_t blocks = (a.rows + each - 1) / each;
+  return blocks < kGridBlocks ? static_cast<uint32_t>(blocks) : walking;
+}
+
 template <typename T, bool ENDS>
 static hipError_t launch_norm_t(const NormArgs& a, const Drop& drop, hipStream_t stream) {
   const RowForm f = norm_form(sizeof(T) == 2, a.cols);
-  const dim3 grid(f.spans ? row_blocks(f, a.rows) : static_cast<uint32_t>(a.rows < 2048 ? a.rows : 2048));
   const dim3 block(f.lanes <= kWave ? kRowThreads : f.lanes);
   constexpr bool kAhead2 = sizeof(T) == 2;  // two float32 spans ahead: too many registers
-  const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, drop);
+  const auto launch = [&](auto kernel, uint32_t blocks) {
+    hipLaunchKernelGGL(kernel, dim3(blocks), block, 0, stream, a, drop);
     return hipGetLastError();
   };
   if (f.lanes < kWave) {
     return with_const<1, 2, 4, 8, 16, 32>(f.lanes, [&](auto lanes) {
       constexpr int G = lanes.value;
       return by_store<T, G, ENDS>(a.rows * a.cols, [&](auto past) {
-        return launch(norm_group_kernel<T, G, ENDS, past.value, 1, true>);
+        return launch(norm_group_kernel<T, G, ENDS, past.value, 1, true>,
+                      norm_blocks<T, ENDS, past.value>(f, a));
       });
     });
   }
   return by_store<T, kWave, ENDS>(a.rows * a.cols, [&](auto past) {
     constexpr bool PAST = past.value;
-    if (f.spans == 0) return launch(norm_wide_kernel<T, ENDS, PAST>);
+    if (f.spans == 0)
+      return launch(norm_wide_kernel<T, ENDS, PAST>, static_cast<uint32_t>(a.rows < 2048 ? a.rows : 2048));
+    const uint32_t blocks = norm_blocks<T, ENDS, PAST>(f, a);
     if (f.lanes == kWave)
-      return f.spans == 1 ? launch(norm_group_kernel<T, kWave, ENDS, PAST, 1, true>)
-                          : launch(norm_group_kernel<T, kWave, ENDS, PAST, 2, kAhead2>);
-    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, ENDS, PAST, 1, true>);
-    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, ENDS, PAST, 2, kAhead2>)
-                          : launch(norm_block_kernel<T, 1024, ENDS, PAST, 2, false>);
+      return f.spans == 1 ? launch(norm_group_kernel<T, kWave, ENDS, PAST, 1, true>, blocks)
+                          : launch(norm_group_kernel<T, kWave, ENDS, PAST, 2, kAhead2>, blocks);
+    if (f.spans == 1) return launch(norm_block_kernel<T, 1024, ENDS, PAST, 1, true>, blocks);
+    return f.lanes <= 512 ? launch(norm_block_kernel<T, 512, ENDS, PAST, 2, kAhead2>, blocks)
+                          : launch(norm_block_kernel<T, 1024, ENDS, PAST, 2, false>, blocks);
   });
 }
 
@@ -480,8 +498,8 @@ hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream
 // ([blocks][2][cols]); sum_parts_kernel adds the blocks' rows in order.  A few
 // rows are one block's, which writes the gradients themselves.
 // Bound by memory: 3 to 5 row arrays.  16384 x 4096 bfloat16 with residual and
-// dropout: 125 us, 5.4 TB/s; 53248 x 128 float32: 22 us (19 and 4 for the parts'
-// sum), 3.8 TB/s.  (Stored past the caches: 3 to 16% slower.)
+// dropout: 125 us, 5.4 TB/s; 53248 x 128 float32: 21 us (18 and 4 for the parts'
+// sum), 3.9 TB/s.  (Stored past the caches: 3 to 16% slower.)
 // ---------------------------------------------------------------------------
 
 // Where a block's sums go: element c of block k's at weight[k * 2 * cols + c] (of

@@ -11,6 +11,7 @@ from __future__ import annotations
 import atexit
 import ctypes
 import functools
+import operator
 import os
 import re
 
@@ -732,6 +733,8 @@ def make_position_buckets(num_buckets, max_distance, bidirectional) -> pss_posit
 _NO_STRIDES = (0, 0, 0)
 
 
+# q_start: an int (operator.index): a tensor or array would be found by its identity,
+# and its value at an earlier call taken.
 @functools.lru_cache(maxsize=256)
 def _scores_params(shape, dtype, table_dtype, q_start, in_strides, out_strides):
     three = ctypes.c_int64 * 3
@@ -776,8 +779,8 @@ def pss_position_bias_forward(table, buckets, out, scores=None, q_start=0, q_sta
                               stream=None):
     """out[b][h][i][k] = scores + table[bucket of query i and key k][h], query i
     of sequence b at position q_start + q_starts[b] + i, key k at k.  out and
-    scores: [B][H][Q][K] (keys contiguous); table: [buckets][H]; q_starts:
-    int32 [B]."""
+    scores: [B][H][Q][K] (keys contiguous); table: [buckets][H]; q_start: an
+    integer of any type, by its value at the call; q_starts: int32 [B]."""
     lib = load_library()
     kind, shape, dtype, dev = _bias_sizes("out", out)
     op, ostr = _scores_of("out", out, shape, dtype, dev)
@@ -787,7 +790,7 @@ def pss_position_bias_forward(table, buckets, out, scores=None, q_start=0, q_sta
     if tkind is None:
         raise TypeError(f"table must be float32 or bfloat16, got {table.dtype}")
     tp = _table_of("table", table, buckets, shape[1], dev)
-    params = _scores_params(shape, kind, tkind, q_start, sstr, ostr)
+    params = _scores_params(shape, kind, tkind, operator.index(q_start), sstr, ostr)
     _check(lib.pss_position_bias_forward(params, ctypes.byref(buckets), tp,
                                          _vector("q_starts", q_starts, torch.int32, shape[0], dev),
                                          sp,
@@ -806,7 +809,7 @@ def pss_position_bias_backward(grad_out, buckets, grad_table, q_start=0, q_start
     if grad_table.dtype is not torch.float32:
         raise TypeError(f"grad_table must be {torch.float32}, got {grad_table.dtype}")
     tp = _table_of("grad_table", grad_table, buckets, shape[1], dev)
-    params = _scores_params(shape, kind, PSS_F32, q_start, gstr, _NO_STRIDES)
+    params = _scores_params(shape, kind, PSS_F32, operator.index(q_start), gstr, _NO_STRIDES)
     _check(lib.pss_position_bias_backward(params, ctypes.byref(buckets),
                                           _vector("q_starts", q_starts, torch.int32, shape[0], dev),
                                           gp, tp, _raw_stream(stream, dev)),

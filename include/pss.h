@@ -434,7 +434,9 @@ int pss_dropout(const pss_rows_params* params, const pss_dropout_params* dropout
  * weight, bias  device, C elements of params->weight_dtype, or NULL
  * eps      > 0, finite
  * s is normalised as float32, before it is rounded for sum_out.  (Squares are
- * float32 too: a row that reaches 1e19 from its mean overflows to rstd = 0.) */
+ * float32 too: a row that reaches 1e19 from its mean overflows to rstd = 0 and
+ * out = bias.  A row's sum has to lie in float32's range: beyond it the mean is
+ * infinite and the row NaN, as one with an infinity or a NaN in it is.) */
 int pss_layer_norm_forward(const pss_rows_params* params, const pss_dropout_params* dropout,
                            const void* x, int64_t x_stride, const void* residual,
                            int64_t residual_stride, const void* weight, const void* bias, float eps,

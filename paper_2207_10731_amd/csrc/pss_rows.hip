@@ -308,7 +308,7 @@ __global__ __launch_bounds__(TH, 4) void norm_block_kernel(const NormArgs a, con
     const float their_mean = other < waves ? lds[turn][0][other] : 0.f;
     const float their_sq = other < waves ? lds[turn][1][other] : 0.f;
     const float mean = group_sum<kMaxWaves>(size * their_mean) * inv;
-    const float away = their_mean - mean;
+    const float away = size > 0.f ? their_mean - mean : 0.f;  // (a square may overflow)
     const float var = group_sum<kMaxWaves>(their_sq + size * (away * away)) * inv;
     const float rstd = 1.f / sqrtf(var + a.eps);
     if (threadIdx.x == 0) norm_store_stats(a, r, mean, rstd);

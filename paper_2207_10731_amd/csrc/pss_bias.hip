@@ -36,8 +36,11 @@ __device__ __forceinline__ int key_rest(int64_t K) {
 // distances of 1024, makes a list of buckets there, a search to each distance and
 // not to each key; farther, keys whose ends share a bucket need two searches.
 // 64 x 16 x 1 x 4096 bfloat16: 7.1 us a call (a search to each key near the query
-// 9.9), 16 x 32 x 1 x 32768: 14.6 us, 4.6 TB/s (19.7); a small call is bound by its
-// launch.
+// 9.9), 16 x 32 x 1 x 32768: 14.6 us, 4.6 TB/s (19.7).  Both are one shape again and
+// again; with a cache that grows by a token a call the first takes 9.4 (the host 7.1
+// us instead of 6.0, and lengths that fill no tile).  Its kernel alone takes 7.6 us,
+// not bound by memory (2.7) but by a chain: start positions, borders, list of
+// buckets, table.
 // ---------------------------------------------------------------------------
 constexpr int kRowPieces = 4;
 
@@ -145,7 +148,9 @@ __global__ __launch_bounds__(kBiasThreads) void bias_row_kernel(const BiasArgs a
 // several (batch, head) pairs, a window of differences to each (as many as leave 2
 // blocks to a CU: 1000 x 8 x 20 x 20 bfloat16 9 us, 19 with 8 blocks to a CU).
 // Bound by memory, the scores read and written: 4 x 16 x 2048 x 2048 bfloat16
-// 174 us, 6.2 TB/s (a bucket search to every element: 1162 us).
+// 174 us, 6.2 TB/s (a bucket search to every element: 1162 us), float32 348 us, 6.2
+// TB/s.  Rows that end inside a vector: 8 x 16 x 511 x 517 bfloat16 43 us, 3.1 TB/s,
+// float32 69 us, 3.9 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kStep = 8;  // queries of a lane
 
@@ -542,7 +547,8 @@ __global__ __launch_bounds__(kBiasThreads) void bias_grad_near_kernel(
 // ---------------------------------------------------------------------------
 // The same for maps with borders farther than that: the window holds the
 // differences of one tile of keys and up to 64 queries, and every tile sums its
-// buckets (512 x 512 scores of 8 x 16 in bfloat16: 44 us, by the form above 23).
+// buckets (8 x 16 x 512 x 512 bfloat16, 64 buckets to distance 3000: 58 us; 32 buckets
+// to 128, by the form above: 21.  4 x 16 x 2048 x 2048: 115 and 93).
 constexpr int kMaxGradRows = 64;  // queries of one group's tile
 
 struct FarShape {

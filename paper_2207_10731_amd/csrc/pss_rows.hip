@@ -79,8 +79,8 @@ __global__ __launch_bounds__(kRowThreads) void dropout_kernel(const RowsIn x, co
 
 // Kernels whose stores gain past the caches: those of whole lines, which a
 // wavefront's bfloat16 rows fill and float32 ones (in two stores, a span's halves)
-// if they are wide (norm of 1048576 x 16 float32: 40 us past them, 32 through
-// them; of 524288 x 64: 47 and 50).
+// if they are wide (norm of 1048576 x 16 float32 without residual: 40 us past them,
+// 32 through them; of 524288 x 64: 47 and 50).
 template <typename T, int G, bool ENDS>
 constexpr bool kGainsPast = sizeof(T) == 2 || G == kWave || (!ENDS && G >= 8);
 // launch(whether the results go past the caches)
@@ -345,7 +345,9 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
 // Wider rows: a block a row, which it reads three times (sum, squares about the
 // mean, result), the last two from L2.  Nothing is stored before the last pass,
 // where every element is read by the lane that then stores its results.  1024 x
-// 30000 float32: 92 us, 2.7 TB/s of the two arrays.
+// 30000 float32: 92 us, 2.7 TB/s of the two arrays, bound by the three reads one
+// after the other (a request in flight to each lane); with residual and dropout 180
+// us, the mask made three times.
 template <typename T, bool ENDS, bool PAST>
 __global__ __launch_bounds__(kRowThreads, 4) void norm_wide_kernel(const NormArgs a, const Drop drop) {
   __shared__ float lds[2 * kRowWaves];
@@ -408,8 +410,9 @@ constexpr int kHeldBf16 = 20;  // of the forward's bfloat16 kernel of one span
 // more rows on a CU but need more registers: bfloat16 takes them for half as many
 // rows again (8192 x 4096: 28 against 34 us; 25000 x 1300, 8 rows against 6: 45
 // against 37), float32, whose spans are twice the bytes, only where a CU would be
-// left with one row (4096 x 8192: 49 against 55 us; 8192 x 4096 with residual, 4 rows
-// against 2: 100 against 94).  Two-span blocks of an odd number of wavefronts leave a
+// left with one row (4096 x 8192: 49 against 55 us; 8192 x 4096 with residual and
+// dropout, 4 rows against 2: 100 against 94; the others without either).  Two-span
+// blocks of an odd number of wavefronts leave a
 // SIMD without its share (8192 x 4104 float32: 5 wavefronts 57 us, 6 54).
 static RowForm norm_form(bool bf16, int64_t cols) {
   const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
@@ -425,8 +428,8 @@ static RowForm norm_form(bool bf16, int64_t cols) {
   return {static_cast<int>(w1) * kWave, 1, static_cast<int>(held)};
 }
 // Blocks that walk rows: what the CUs hold, with as many rows to each (a last
-// round of a few rows takes as long as the others: 16000 x 2500 float32 55 against
-// 57 us).  Narrow rows, many to a block, fill the CUs instead (backward of 53248 x
+// round of a few rows takes as long as the others: norm of 16000 x 2500 float32
+// without residual 55 against 57 us).  Narrow rows, many to a block, fill the CUs instead (backward of 53248 x
 // 128 float32 20.9 against 21.6 us).
 static uint32_t row_blocks(const RowForm& f, int64_t rows) {
   const bool group = f.lanes <= kWave;
@@ -498,8 +501,9 @@ hipError_t launch_norm(bool bf16, const NormArgs& a, const Drop& drop, hipStream
 // ([blocks][2][cols]); sum_parts_kernel adds the blocks' rows in order.  A few
 // rows are one block's, which writes the gradients themselves.
 // Bound by memory: 3 to 5 row arrays.  16384 x 4096 bfloat16 with residual and
-// dropout: 125 us, 5.4 TB/s; 53248 x 128 float32: 21 us (18 and 4 for the parts'
-// sum), 3.9 TB/s.  (Stored past the caches: 3 to 16% slower.)
+// dropout: 125 us, 5.4 TB/s (122 and 5 for the parts' sum in calls one after the other;
+// 105 for a first one, before whose stores none wait to reach memory); 53248 x 128
+// float32: 21 us (18 and 4), 3.9 TB/s.  (Stored past the caches: 3 to 16% slower.)
 // ---------------------------------------------------------------------------
 
 // Where a block's sums go: element c of block k's at weight[k * 2 * cols + c] (of
@@ -727,7 +731,9 @@ __global__ __launch_bounds__(TH) void norm_grad_block_kernel(const NormGradArgs 
   }
 }
 
-// Wider rows.  First the rows' two means (m1 and m2, [2][rows] of scratch) ...
+// Wider rows, which are read twice (2048 x 16384 float32 without residual: 123 us, 3.3
+// TB/s of the three arrays).  First the rows' two means (m1 and m2, [2][rows] of
+// scratch) ...
 template <typename T, bool ENDS>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_means_kernel(const NormGradArgs a,
                                                                       float* __restrict__ means) {
@@ -843,10 +849,10 @@ __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(const float* __r
 }
 
 // One span a lane takes up to 128 registers, two bfloat16 ones up to 170: blocks of
-// two are for rows that one span does not cover (4000 x 9000 bfloat16: 59 us, the
-// wide form 91; float32 they would spill, 217 against 208 with residual).  Five
-// wavefronts a block leave a SIMD without its share: 6 (16000 x 2500 bfloat16: 70
-// against 86 us).
+// two are for rows that one span does not cover (4000 x 9000 bfloat16 without
+// residual: 56 us, the wide form 91; float32 they would spill, 217 against 208 with
+// residual and dropout).  Five wavefronts a block leave a SIMD without its share: 6
+// (16000 x 2500 bfloat16 without residual: 69 against 86 us).
 constexpr int kGradWaves2 = 12;
 static RowForm grad_form(bool bf16, int64_t cols) {
   const int64_t n = (cols + kLanePiece - 1) / kLanePiece;
@@ -927,8 +933,9 @@ hipError_t launch_norm_grad(bool bf16, const NormGradArgs& a, const Drop& drop, 
     return launch_norm_grad_t<decltype(t), ends.value>(a, drop, sums, means, parts, stream);
   });
   if (e == hipSuccess && join) {
-    // whole lines of columns where they leave enough blocks (16384 x 2048 bfloat16:
-    // 43.0 against 45.5 us for the call; 3000 x 1000: 12.2 against 11.9)
+    // whole lines of columns where they leave enough blocks (16384 x 2048 bfloat16
+    // without residual: 43.0 against 45.5 us for the call; 3000 x 1000: 12.2 against
+    // 11.9)
     e = with_const<16, 32>(a.cols >= kWideSums ? 32 : 16, [&](auto wide) {
       constexpr int COLS = wide.value;
       const int64_t blocks = (2 * a.cols + COLS - 1) / COLS;

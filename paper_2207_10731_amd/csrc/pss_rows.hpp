@@ -460,11 +460,22 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
 
-// Results of more than this are stored past the caches.  Alone such a call gains 3 to
-// 15% (bias of 2 x 16 x 2048 x 2048 bfloat16 88 against 94 us, norm of 262144 x 128
-// float32 47 against 50); where the next call reads its results, the two together
-// lose 2% at 64 MB (norm, then dropout: 49.4 against 48.3 us) and gain 1 to 8% at
-// 512 MB; below 64 MB a program has the results in the caches next.
+// Results of more than this are stored past the caches.  The call itself gains 3 to 13%
+// at nearly every size; a next call that reads the results loses as long as the
+// memory-side cache (256 MB) would have held them.  Which of the two a program has the library
+// cannot see; below 64 MB the results are taken to be read next.  us through / past
+// the caches by the size of one result, rows of 4096 bfloat16, scores 512 x 1024:
+//                                   72 MB        128 MB       256 MB       512 MB
+//   norm                         30.0 / 28.6  50.0 / 47.6   102 / 95     193 / 184
+//   norm, dropout of its result  53.3 / 54.6  88.3 / 90.9   173 / 178    373 / 350
+//   residual, dropout, norm      57.5 / 55.7   104 / 100    212 / 204    455 / 428
+//   the same, norm of both       94.1 / 98.1   162 / 172    353 / 348    771 / 724
+//   dropout                      28.0 / 25.3  48.3 / 42.7   92.8 / 82.3  181 / 163
+//   dropout, norm of its result  54.5 / 54.6  90.9 / 90.7   180 / 174    382 / 355
+//   position bias                             48.4 / 46.4   94.4 / 89.6  187 / 176
+//   bias, its table's gradient                72.0 / 78.9   133 / 144    276 / 270
+// (Float32 gains 3 to 19% alone; its chains lose up to 7% at 72 and 128 MB, lie between
+// 7% slower and 10% faster at 256 and gain from 384 on.)
 constexpr int64_t kPastBytes = int64_t{64} << 20;
 
 // f(the constant that n equals); n is one of them.

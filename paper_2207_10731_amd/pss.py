@@ -733,8 +733,14 @@ def make_position_buckets(num_buckets, max_distance, bidirectional) -> pss_posit
 _NO_STRIDES = (0, 0, 0)
 
 
-# q_start: an int (operator.index): a tensor or array would be found by its identity,
-# and its value at an earlier call taken.
+def _position(q_start):
+    """The first query's position as an int.  (A tensor or array would be found among
+    the kept blocks by its identity, and its value at an earlier call taken.)  One
+    beyond 32 bits goes on as one that the library refuses, not modulo 2^64."""
+    q = operator.index(q_start)
+    return q if 0 <= q < 2**31 else -1
+
+
 @functools.lru_cache(maxsize=256)
 def _scores_params(shape, dtype, table_dtype, q_start, in_strides, out_strides):
     three = ctypes.c_int64 * 3
@@ -790,7 +796,7 @@ def pss_position_bias_forward(table, buckets, out, scores=None, q_start=0, q_sta
     if tkind is None:
         raise TypeError(f"table must be float32 or bfloat16, got {table.dtype}")
     tp = _table_of("table", table, buckets, shape[1], dev)
-    params = _scores_params(shape, kind, tkind, operator.index(q_start), sstr, ostr)
+    params = _scores_params(shape, kind, tkind, _position(q_start), sstr, ostr)
     _check(lib.pss_position_bias_forward(params, ctypes.byref(buckets), tp,
                                          _vector("q_starts", q_starts, torch.int32, shape[0], dev),
                                          sp,
@@ -809,7 +815,7 @@ def pss_position_bias_backward(grad_out, buckets, grad_table, q_start=0, q_start
     if grad_table.dtype is not torch.float32:
         raise TypeError(f"grad_table must be {torch.float32}, got {grad_table.dtype}")
     tp = _table_of("grad_table", grad_table, buckets, shape[1], dev)
-    params = _scores_params(shape, kind, PSS_F32, operator.index(q_start), gstr, _NO_STRIDES)
+    params = _scores_params(shape, kind, PSS_F32, _position(q_start), gstr, _NO_STRIDES)
     _check(lib.pss_position_bias_backward(params, ctypes.byref(buckets),
                                           _vector("q_starts", q_starts, torch.int32, shape[0], dev),
                                           gp, tp, _raw_stream(stream, dev)),

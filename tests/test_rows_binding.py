@@ -89,3 +89,21 @@ def test_decode_loop_with_a_counter_in_place():
         pss.pss_position_bias_backward(scores, m, h, q_start=p)
         assert torch.equal(g, h)
         pos += 1
+
+
+@pytest.mark.parametrize("call", [_forward, _backward])
+@pytest.mark.parametrize("far", [2**64 + 5, 2**64, -2**64 + 7, 2**32, 2**63, -1])
+def test_positions_out_of_range_stay_so(call, far, starts):
+    """What the library gets is refused there, not a position modulo 2^64."""
+    call(far)
+    assert not 0 <= starts[0] <= 2**29
+
+
+@pytest.mark.gpu
+def test_positions_out_of_range_are_refused():
+    m, x = pss.make_position_buckets(8, 64, True), torch.zeros(2, 3, 4, 5, device="cuda")
+    for far in (2**64 + 5, -1, 2**29 + 1):
+        with pytest.raises(pss.PssError):
+            pss.pss_position_bias_forward(torch.zeros(8, 3, device="cuda"), m, x, q_start=far)
+        with pytest.raises(pss.PssError):
+            pss.pss_position_bias_backward(x, m, torch.zeros(8, 3, device="cuda"), q_start=far)

@@ -116,3 +116,12 @@ def test_few_queries_of_far_borders(Q, K, start, borders, both, dtype):
     pss.pss_position_bias_forward(table, m, x, scores=x, q_start=start,
                                   q_starts=torch.from_numpy(starts).cuda())
     assert torch.equal(x, both_sum)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("K", [1, 2, 3, 4, 5, 7, 8, 9, 15])
+def test_gradient_of_rows_of_few_keys(K, dtype):
+    """Rows shorter than a vector, of one and just above, near and far borders."""
+    for borders, both in ((USUAL, True), ([0, 3, 2000], True), ([0, 1, 5, 1100], False)):
+        for B, H, Q, start, per in ((3, 2, 70, 0, True), (1, 3, 1, 1102, False), (50, 1, 9, 1095, False)):
+            _exact(_map(borders, both), B, H, Q, K, dtype, start, per, 0, K)
